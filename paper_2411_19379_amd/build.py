@@ -1,4 +1,4 @@
-"""Build the HIP library (gfx950) in-tree with hipcc, and the host-only prefix-cache library with g++."""
+"""Build the HIP libraries (gfx950) in-tree with hipcc, and the host-only prefix-cache library with g++."""
 from __future__ import annotations
 
 import os
@@ -41,6 +41,20 @@ def build_prefix_cache(verbose: bool = False) -> str:
     return CACHE_LIB_PATH
 
 
+ATTN_LIB_PATH = os.path.join(_PKG, "libattn_cache.so")
+ATTN_SOURCES = ["attn_api.hip", "attn_step.hip", "attn_attend.hip"]
+
+
+def build_attention(verbose: bool = False) -> str:
+    """The attention layers' operators: a library of their own, like the prefix cache whose keys and values they keep."""
+    srcs = [os.path.join(CSRC, s) for s in ATTN_SOURCES]
+    cmd = ["hipcc", *HIPCC_FLAGS, "-I", os.path.join(_ROOT, "include"), "-I", CSRC, "-o", ATTN_LIB_PATH, *srcs]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return ATTN_LIB_PATH
+
+
 PEAK_PROBE_PATH = os.path.join(_PKG, "peak_probe")
 
 
@@ -57,4 +71,5 @@ def build_peak_probe(verbose: bool = False) -> str:
 if __name__ == "__main__":
     build_library(verbose=True)
     build_prefix_cache(verbose=True)
+    build_attention(verbose=True)
     build_peak_probe(verbose=True)

@@ -1,0 +1,1033 @@
+// Attention of the new tokens of a packed batch over the paged cache: for chunks of prompts, for single tokens, and in fp32.
+//
+// One pass over the keys with a running maximum m and weight l per row:  p = 2^(c (s - m)),  l = sum p,  O = sum p v,  with
+// c = scale log2(e); when a row's scores outgrow m, what has been summed is scaled down.  A query head reads the key head of
+// its group, so the rows of a sequence are (token, head of the group) pairs: all that read one key head.
+//
+// All three kernels compute S^T = K Q^T, keys down the matrix rows, so that a lane holds scores of one row of the problem and
+// keeps that row's m and l in registers, and O^T = V^T P^T, of which the lane's accumulators are the same row again.  The
+// accumulators of S^T are, packed, already the operand P^T of the second product, with the keys in an order that the operand
+// V^T is read in as well: P never leaves the registers.
+//
+// Rows that see only part of a tile of keys take their weights of the others as zero, and V's infinities and NaN in such
+// tiles stay out of the matrix product (0 * inf is not 0): they are added to the rows that see them one key at a time.
+#include "attn_common.h"
+
+#ifndef ATTN_TARGET  // workgroups that a launch is dealt to, where tests do not choose them
+#define ATTN_TARGET 0
+#endif
+
+namespace {
+
+constexpr float kOutgrown = 8.f;  // powers of two by which a weight may exceed 1 before its row is scaled down
+
+template <typename E> __device__ __forceinline__ void unpack4(uint2 u, float *v)
+{
+    v[0] = E::lo(u.x), v[1] = E::hi(u.x), v[2] = E::lo(u.y), v[3] = E::hi(u.y);
+}
+
+// ================================================================ chunks
+// A workgroup takes 32 rows per wave and walks the keys in tiles of 64, K and V in LDS in two buffers: while a tile is worked
+// on, the next one is on its way in registers.
+constexpr int kChunkKeys = 64;
+
+template <int D> struct ChunkTile {
+    static constexpr int kPieces = D / 8;  // 16-byte pieces of a row
+    static constexpr int kBytes = kChunkKeys * D * 2;
+    // Where piece c of row r lies.  K is read 32 rows at a piece, V 8 rows at four neighbouring pieces: both without two lanes
+    // of a group on one bank.
+    static __device__ __forceinline__ int k_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) << 4); }
+    static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)) << 4); }
+};
+
+template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) void attn_chunk_kernel(AttendArgs a)
+{
+    typedef ChunkTile<D> Tile;
+    constexpr int NT = 64 * NW, ROWS = 32 * NW, PIECES = Tile::kPieces;
+    constexpr int LOADS = kChunkKeys * PIECES / NT;  // pieces of K (and of V) per thread and tile
+    constexpr int ROWS_PER_LOAD = NT / PIECES;
+    static_assert(LOADS * NT == kChunkKeys * PIECES && PIECES <= 64, "whole tiles");
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    unsigned char *const lds_k = lds_raw, *const lds_v = lds_raw + 2 * Tile::kBytes;
+    int *const lds_flag = reinterpret_cast<int *>(lds_raw + 4 * Tile::kBytes);  // [2][64]: bit 0 the key exists, bit 1 its V is not finite
+    int *const lds_item = lds_flag + 2 * kChunkKeys;
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), half = l / 32;
+    const int kv_head = blockIdx.x % a.Hkv;
+    Item it;
+    if (!find_item<NT, ROWS, kChunkKeys>(a, blockIdx.x / a.Hkv, false, lds_item, &it))
+        return;
+    const Seq s = load_seq(a, it.seq);
+    const int r0 = it.tile * ROWS;
+    const KeyRange keys = key_range<kChunkKeys>(a, s, r0, ROWS);
+    const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
+    const int end = keys.pos1 + 1;  // no row of the workgroup sees a key behind it
+
+    // this lane's row
+    const int row = r0 + 32 * wave + l % 32;
+    const bool wave_works = r0 + 32 * wave < s.rows, row_works = row < s.rows;
+    const int token = row_works ? row / a.group : 0, head = kv_head * a.group + (row_works ? row - token * a.group : 0);
+    const int pos = s.cached + token;
+    const int wave_last = r0 + 32 * wave + 31 < s.rows ? r0 + 32 * wave + 31 : s.rows - 1;
+    const int wave_pos0 = s.cached + (wave_works ? (r0 + 32 * wave) / a.group : 0);
+    const int wave_pos1 = s.cached + (wave_works ? wave_last / a.group : 0);
+    uint4 qf[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        qf[ks] = make_uint4(0, 0, 0, 0);
+        if (row_works)
+            qf[ks] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + (int64_t)(s.start + token) * a.q_stride +
+                                                      (int64_t)head * D + ks * 16 + 8 * half);
+    }
+
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+        o[db] = zero16();
+    float m = -INFINITY, lsum = 0.f;
+    bool seen = false;
+
+    // what this thread loads: rows load_row + i * ROWS_PER_LOAD, piece load_piece
+    const int load_row = tid / PIECES, load_piece = tid % PIECES;
+    uint4 kreg[LOADS], vreg[LOADS];
+    int block[LOADS];
+    int there = 0;  // bit i: the key exists
+    auto look_up = [&](int step) {  // the blocks of a tile's rows
+        const int j0 = keys.tile(step) * kChunkKeys;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            block[i] = step < step_end ? table_entry(a, it.seq, j0 + load_row + i * ROWS_PER_LOAD, end) : -1;
+    };
+    auto request = [&](int step) {
+        const int j0 = keys.tile(step) * kChunkKeys;
+        there = 0;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = cache_row(a, block[i], kv_head, j0 + load_row + i * ROWS_PER_LOAD);
+            kreg[i] = vreg[i] = make_uint4(0, 0, 0, 0);
+            if (r >= 0) {
+                const int64_t at = (int64_t)r * D + load_piece * 8;
+                kreg[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.k_cache) + at);
+                vreg[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.v_cache) + at);
+                there |= 1 << i;
+            }
+        }
+    };
+
+    if (step_begin < step_end) {
+        look_up(step_begin);
+        request(step_begin);
+        look_up(step_begin + 1);
+    }
+    for (int step = step_begin; step < step_end; ++step) {
+        const int buf = step & 1, j0 = keys.tile(step) * kChunkKeys;
+        unsigned char *const kt = lds_k + buf * Tile::kBytes, *const vt = lds_v + buf * Tile::kBytes;
+        int *const flag = lds_flag + buf * kChunkKeys;
+        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kChunkKeys);  // by the workgroup
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = load_row + i * ROWS_PER_LOAD;
+            bool bad = false;
+            if (part_seen) {
+                bad = drop_not_finite<E>(vreg[i].x) || bad;
+                bad = drop_not_finite<E>(vreg[i].y) || bad;
+                bad = drop_not_finite<E>(vreg[i].z) || bad;
+                bad = drop_not_finite<E>(vreg[i].w) || bad;
+            }
+            const uint64_t any = __ballot(bad);
+            const uint64_t of_row = any >> (l / PIECES * PIECES) & ((1ull << (PIECES - 1) << 1) - 1);
+            *reinterpret_cast<uint4 *>(kt + Tile::k_at(r, load_piece)) = kreg[i];
+            *reinterpret_cast<uint4 *>(vt + Tile::v_at(r, load_piece)) = vreg[i];
+            if (load_piece == 0)
+                flag[r] = (there >> i & 1) | (of_row != 0 ? 2 : 0);
+        }
+        if (step + 1 < step_end) {
+            request(step + 1);
+            look_up(step + 2);
+        }
+        lds_barrier();
+        if (!wave_works)
+            continue;
+
+        f32x16 st[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            st[kb] = zero16();
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const uint4 kf = *reinterpret_cast<const uint4 *>(kt + Tile::k_at(kb * 32 + l % 32, 2 * ks + half));
+                st[kb] = E::mfma32(kf, qf[ks], st[kb]);
+            }
+        }
+        const int f = flag[l];
+        const uint64_t exist = __ballot((f & 1) != 0), bad = __ballot((f & 2) != 0);
+        const bool partly = !all_see(a, wave_pos0, wave_pos1, j0, kChunkKeys) || exist != ~0ull;
+        uint32_t hidden = 0;  // bit 16 kb + r: the row does not see that key
+        if (partly) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = kb * 32 + 8 * (r / 4) + 4 * half + r % 4;
+                    const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos, j0 + key);
+                    hidden |= sees_it ? 0u : 1u << (16 * kb + r);
+                    if (!sees_it)
+                        st[kb][r] = -INFINITY;
+                }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                top = fmaxf(top, st[kb][r]);
+        seen = seen || hidden != 0xffffffffu;
+        if (__any(top > m + kOutgrown / a.scale_log2)) {
+            const float both = fmaxf(top, read_from(top, l ^ 32)), next = fmaxf(m, both);
+            const float down = next == m ? 1.f : exp2_fast((m - next) * a.scale_log2);
+            m = next;
+            lsum *= down;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    o[db][r] *= down;
+        }
+        const float mc = finite_max(m) * a.scale_log2;
+        uint4 pf[4];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            float p[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                p[r] = exp2_fast(__builtin_fmaf(st[kb][r], a.scale_log2, -mc));
+                if (partly && (hidden >> (16 * kb + r) & 1))
+                    p[r] = 0.f;  // also where m is infinite
+                lsum += p[r];
+                st[kb][r] = p[r];
+            }
+            pf[2 * kb] = make_uint4(E::pack(p[0], p[1]), E::pack(p[2], p[3]), E::pack(p[4], p[5]), E::pack(p[6], p[7]));
+            pf[2 * kb + 1] = make_uint4(E::pack(p[8], p[9]), E::pack(p[10], p[11]), E::pack(p[12], p[13]), E::pack(p[14], p[15]));
+        }
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const int r_lo = 16 * kk + 4 * half + (l % 16) / 4;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                const int c = db * 4 + 2 * (l / 16 % 2) + (l % 4) / 2;
+                const uint4 vf = lds_frag_tr(vt + Tile::v_at(r_lo, c) + 8 * (l % 2), vt + Tile::v_at(r_lo + 8, c) + 8 * (l % 2));
+                o[db] = E::mfma32(vf, pf[kk], o[db]);
+            }
+        }
+        if (bad != 0) {
+            for (uint64_t left = bad; left != 0; left &= left - 1) {
+                const int key = __builtin_ctzll(left), r = 4 * (key % 32 / 8) + key % 4, from = key % 8 / 4;
+                float p = 0.f;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        p = 16 * kb + e == 16 * (key / 32) + r ? st[kb][e] : p;
+                p = read_from(p, l % 32 + 32 * from);
+                const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
+                const bool sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key);
+                const uint16_t *v_row = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float v[4];
+                        unpack4<E>(*reinterpret_cast<const uint2 *>(v_row + db * 32 + 8 * q + 4 * half), v);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[db][4 * q + e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
+                    }
+            }
+        }
+    }
+    if (!wave_works)
+        return;
+    lsum += read_from(lsum, l ^ 32);
+    const int seen_there = read_from((int)seen, l ^ 32);
+    seen = seen || seen_there != 0;
+    const float w = row_weight(lsum, m, seen);
+    if (!row_works)
+        return;
+    if (it.n_splits > 1) {
+        const int part = part_of(a, it, kv_head, it.split);
+        if (part >= a.most_parts)
+            return;
+        const int64_t at = (int64_t)part * a.rows_cap + row - r0;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<float4 *>(a.part + at * D + db * 32 + 8 * q + 4 * half) =
+                    make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
+        if (half == 0)
+            *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(m, w);
+        return;
+    }
+    const float scale = w == 0.f ? 0.f : w < 0.f ? NAN : 1.f / w;
+    uint16_t *const out = static_cast<uint16_t *>(a.out) + (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint2 *>(out + db * 32 + 8 * q + 4 * half) =
+                make_uint2(E::pack(o[db][4 * q] * scale, o[db][4 * q + 1] * scale), E::pack(o[db][4 * q + 2] * scale, o[db][4 * q + 3] * scale));
+    if (a.lse && half == 0)
+        a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
+}
+
+// ================================================================ few rows
+// For the rows of single tokens, 16 RB of them at a time: each of the four waves takes every fourth tile of 32 keys, K from
+// memory right into the operand's registers, V through LDS of its own for the transposing reads; no barriers until the waves'
+// results are joined.  What bounds it is reading the cache: a wave's next tile is requested before the present one is used.
+constexpr int kFewKeys = 32;
+constexpr int kFewWaves = 4;
+
+template <int D> struct FewTile {
+    static constexpr int kPieces = D / 8;
+    static constexpr int kBytes = kFewKeys * D * 2;
+    // V is read 16 rows at two neighbouring pieces
+    static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4); }
+};
+
+template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves, 2) void attn_few_kernel(AttendArgs a)
+{
+    typedef FewTile<D> Tile;
+    constexpr int NT = 64 * kFewWaves, ROWS = 16 * RB, PIECES = Tile::kPieces;
+    constexpr int KS = D / 32;                         // products of a block of scores
+    constexpr int V_LOADS = kFewKeys * PIECES / 64;    // pieces of V per lane
+    constexpr int V_ROWS = 64 / PIECES;                // rows per such load
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), quarter = l / 16;
+    unsigned char *const vt = lds_raw + wave * Tile::kBytes;
+
+    const int kv_head = blockIdx.x % a.Hkv;
+    Item it;
+    if (!find_item<NT, ROWS, kFewKeys>(a, blockIdx.x / a.Hkv, false, reinterpret_cast<int *>(lds_raw), &it))
+        return;
+    const Seq s = load_seq(a, it.seq);
+    const int r0 = it.tile * ROWS;
+    const KeyRange keys = key_range<kFewKeys>(a, s, r0, ROWS);
+    const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
+    const int end = keys.pos1 + 1;
+
+    int pos[RB], token[RB], head[RB];
+    bool row_works[RB];
+    uint4 qf[RB][KS];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = r0 + 16 * rb + l % 16;
+        row_works[rb] = row < s.rows;
+        token[rb] = row_works[rb] ? row / a.group : 0;
+        head[rb] = kv_head * a.group + (row_works[rb] ? row - token[rb] * a.group : 0);
+        pos[rb] = s.cached + token[rb];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            qf[rb][ks] = make_uint4(0, 0, 0, 0);
+            if (row_works[rb])
+                qf[rb][ks] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + (int64_t)(s.start + token[rb]) * a.q_stride +
+                                                              (int64_t)head[rb] * D + ks * 32 + 8 * quarter);
+        }
+    }
+    f32x4 o[RB][D / 16];
+    float m[RB], lsum[RB];
+    bool seen[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        m[rb] = -INFINITY, lsum[rb] = 0.f, seen[rb] = false;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db)
+            o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    lds_barrier();  // the words of find_item have been read
+
+    uint4 kreg[2][KS], vreg[V_LOADS];
+    int block = -1, row_of_key = -1;  // of key l % 32 of a tile: of the one behind the next, of the next
+    uint64_t exist_next = 0;
+    auto look_up = [&](int step) { block = step < step_end ? table_entry(a, it.seq, keys.tile(step) * kFewKeys + l % 32, end) : -1; };
+    auto request = [&](int step) {
+        row_of_key = cache_row(a, block, kv_head, keys.tile(step) * kFewKeys + l % 32);
+        exist_next = __ballot(row_of_key >= 0);
+        const uint16_t *const k = static_cast<const uint16_t *>(a.k_cache), *const v = static_cast<const uint16_t *>(a.v_cache);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int r = read_from(row_of_key, 16 * kb + l % 16);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                kreg[kb][ks] = make_uint4(0, 0, 0, 0);
+                if (r >= 0)
+                    kreg[kb][ks] = *reinterpret_cast<const uint4 *>(k + (int64_t)r * D + ks * 32 + 8 * quarter);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < V_LOADS; ++i) {
+            const int r = read_from(row_of_key, i * V_ROWS + l / PIECES);
+            vreg[i] = make_uint4(0, 0, 0, 0);
+            if (r >= 0)
+                vreg[i] = *reinterpret_cast<const uint4 *>(v + (int64_t)r * D + l % PIECES * 8);
+        }
+    };
+    if (step_begin + wave < step_end) {
+        look_up(step_begin + wave);
+        request(step_begin + wave);
+        look_up(step_begin + wave + kFewWaves);
+    }
+    for (int step = step_begin + wave; step < step_end; step += kFewWaves) {
+        const int j0 = keys.tile(step) * kFewKeys;
+        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kFewKeys);
+        const uint32_t exist = (uint32_t)exist_next;
+        f32x4 st[RB][2];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                st[rb][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    st[rb][kb] = E::mfma16(kreg[kb][ks], qf[rb][ks], st[rb][kb]);
+            }
+        uint32_t bad = 0;  // keys whose V is not finite
+        if (part_seen) {
+#pragma unroll
+            for (int i = 0; i < V_LOADS; ++i) {
+                bool b = drop_not_finite<E>(vreg[i].x);
+                b = drop_not_finite<E>(vreg[i].y) || b;
+                b = drop_not_finite<E>(vreg[i].z) || b;
+                b = drop_not_finite<E>(vreg[i].w) || b;
+                const uint64_t any = __ballot(b);
+#pragma unroll
+                for (int r = 0; r < V_ROWS; ++r)
+                    bad |= (any >> (r * PIECES) & ((1ull << PIECES) - 1)) != 0 ? 1u << (i * V_ROWS + r) : 0u;
+            }
+        }
+        lds_wait();  // the reads of the tile in front are done
+#pragma unroll
+        for (int i = 0; i < V_LOADS; ++i)
+            *reinterpret_cast<uint4 *>(vt + Tile::v_at(i * V_ROWS + l / PIECES, l % PIECES)) = vreg[i];
+        if (step + kFewWaves < step_end) {
+            request(step + kFewWaves);
+            look_up(step + 2 * kFewWaves);
+        }
+        const bool partly = part_seen || exist != 0xffffffffu;
+        uint4 pf[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            uint32_t hidden = 0;
+            if (partly) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = kb * 16 + 4 * quarter + r;
+                        const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos[rb], j0 + key);
+                        hidden |= sees_it ? 0u : 1u << (4 * kb + r);
+                        if (!sees_it)
+                            st[rb][kb][r] = -INFINITY;
+                    }
+            }
+            seen[rb] = seen[rb] || hidden != 0xffu;
+            float top = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    top = fmaxf(top, st[rb][kb][r]);
+            if (__any(top > m[rb] + kOutgrown / a.scale_log2)) {
+                top = fmaxf(top, read_from(top, l ^ 16));
+                top = fmaxf(top, read_from(top, l ^ 32));
+                const float next = fmaxf(m[rb], top), down = next == m[rb] ? 1.f : exp2_fast((m[rb] - next) * a.scale_log2);
+                m[rb] = next;
+                lsum[rb] *= down;
+#pragma unroll
+                for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        o[rb][db][r] *= down;
+            }
+            const float mc = finite_max(m[rb]) * a.scale_log2;
+            float p[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = exp2_fast(__builtin_fmaf(st[rb][e / 4][e % 4], a.scale_log2, -mc));
+                if (partly && (hidden >> e & 1))
+                    p[e] = 0.f;
+                lsum[rb] += p[e];
+                st[rb][e / 4][e % 4] = p[e];
+            }
+            pf[rb] = make_uint4(E::pack(p[0], p[1]), E::pack(p[2], p[3]), E::pack(p[4], p[5]), E::pack(p[6], p[7]));
+        }
+        lds_wait();  // V is there
+        const int r_lo = 4 * quarter + (l % 16) / 4;
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) {
+            const int c = db * 2 + (l % 4) / 2;
+            const uint4 vf = lds_frag_tr(vt + Tile::v_at(r_lo, c) + 8 * (l % 2), vt + Tile::v_at(r_lo + 16, c) + 8 * (l % 2));
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                o[rb][db] = E::mfma16(vf, pf[rb], o[rb][db]);
+        }
+        for (uint32_t left = bad; left != 0; left &= left - 1) {
+            const int key = __builtin_ctz(left), e_of = 4 * (key / 16) + key % 4, from = key % 16 / 4;
+            const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
+            const uint16_t *v_row = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                float p = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    p = e == e_of ? st[rb][e / 4][e % 4] : p;
+                p = read_from(p, l % 16 + 16 * from);
+                const bool sees_it = row_works[rb] && cr >= 0 && sees(a, pos[rb], j0 + key);
+#pragma unroll
+                for (int db = 0; db < D / 16; ++db) {
+                    float v[4];
+                    unpack4<E>(*reinterpret_cast<const uint2 *>(v_row + db * 16 + 4 * quarter), v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[rb][db][e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
+                }
+            }
+        }
+    }
+
+    // the four waves' results, 16 rows at a time
+    lds_barrier();
+    float *const lds_o = reinterpret_cast<float *>(lds_raw);            // [wave][16][D + 4]
+    float *const lds_ml = lds_o + kFewWaves * 16 * (D + 4);             // [wave][16][2]
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        float w = lsum[rb];
+        w += read_from(w, l ^ 16);
+        w += read_from(w, l ^ 32);
+        int any = (int)seen[rb];
+        any |= read_from(any, l ^ 16);
+        any |= read_from(any, l ^ 32);
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db)
+            *reinterpret_cast<float4 *>(lds_o + (wave * 16 + l % 16) * (D + 4) + db * 16 + 4 * quarter) =
+                make_float4(o[rb][db][0], o[rb][db][1], o[rb][db][2], o[rb][db][3]);
+        if (quarter == 0)
+            *reinterpret_cast<float2 *>(lds_ml + (wave * 16 + l) * 2) = make_float2(m[rb], row_weight(w, m[rb], any != 0));
+        lds_barrier();
+        // thread: row tid / 16, values 4 (tid % 16) and every 64 behind them
+        const int row = tid / 16, full_row = r0 + 16 * rb + row;
+        if (full_row < s.rows) {
+            JoinedRow j;
+#pragma unroll
+            for (int w2 = 0; w2 < kFewWaves; ++w2)
+                j.add_max(lds_ml[(w2 * 16 + row) * 2]);
+            float part_w[kFewWaves];
+#pragma unroll
+            for (int w2 = 0; w2 < kFewWaves; ++w2)
+                part_w[w2] = j.add_weight(lds_ml[(w2 * 16 + row) * 2], lds_ml[(w2 * 16 + row) * 2 + 1], a.scale_log2);
+            const int tok = full_row / a.group, hd = kv_head * a.group + full_row - tok * a.group;
+            const int part = it.n_splits > 1 ? part_of(a, it, kv_head, it.split) : 0;
+            if (part < a.most_parts || it.n_splits == 1) {
+                const int64_t at = (int64_t)part * a.rows_cap + 16 * rb + row;
+                const float scale = it.n_splits > 1 ? 1.f : j.scale();
+#pragma unroll
+                for (int d = 4 * (tid % 16); d < D; d += 64) {
+                    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int w2 = 0; w2 < kFewWaves; ++w2) {
+                        const float4 x = *reinterpret_cast<const float4 *>(lds_o + (w2 * 16 + row) * (D + 4) + d);
+                        if (part_w[w2] != 0.f) {
+                            v[0] += part_w[w2] * x.x, v[1] += part_w[w2] * x.y, v[2] += part_w[w2] * x.z, v[3] += part_w[w2] * x.w;
+                        }
+                    }
+                    if (it.n_splits > 1)
+                        *reinterpret_cast<float4 *>(a.part + at * D + d) = make_float4(v[0], v[1], v[2], v[3]);
+                    else
+                        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + (int64_t)(s.start + tok) * a.out_stride + (int64_t)hd * D + d) =
+                            make_uint2(E::pack(v[0] * scale, v[1] * scale), E::pack(v[2] * scale, v[3] * scale));
+                }
+                if (tid % 16 == 0) {
+                    if (it.n_splits > 1)
+                        *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(j.m, j.weight());
+                    else if (a.lse)
+                        a.lse[(int64_t)(s.start + tok) * a.Hq + hd] = row_lse(j.m, j.weight(), a.scale_log2);
+                }
+            }
+        }
+        lds_barrier();
+    }
+}
+
+// ================================================================ fp32
+// 16 rows per wave, 64 per workgroup, keys in tiles of 32 through LDS; products on the fp32 matrix instructions, which bound
+// it (a sixteenth of the 16-bit rate).
+constexpr int kF32Keys = 32;
+constexpr int kF32Waves = 4;
+
+template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_kernel(AttendArgs a)
+{
+    constexpr int NT = 64 * kF32Waves, ROWS = 16 * kF32Waves;
+    constexpr int PIECES = D / 4, LOADS = kF32Keys * PIECES / NT, ROWS_PER_LOAD = NT / PIECES;
+    constexpr int STRIDE = D + 4;  // floats; rows four apart start 16 banks apart
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    float *const kt = reinterpret_cast<float *>(lds_raw), *const vt = kt + kF32Keys * STRIDE;
+    int *const flag = reinterpret_cast<int *>(vt + kF32Keys * STRIDE);  // [32]
+    int *const lds_bad = flag + kF32Keys;                               // [32]
+    int *const lds_item = lds_bad + kF32Keys;
+
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), quarter = l / 16;
+    const int kv_head = blockIdx.x % a.Hkv;
+    Item it;
+    if (!find_item<NT, ROWS, kF32Keys>(a, blockIdx.x / a.Hkv, false, lds_item, &it))
+        return;
+    const Seq s = load_seq(a, it.seq);
+    const int r0 = it.tile * ROWS;
+    const KeyRange keys = key_range<kF32Keys>(a, s, r0, ROWS);
+    const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
+    const int end = keys.pos1 + 1;
+
+    const int row = r0 + 16 * wave + l % 16;
+    const bool wave_works = r0 + 16 * wave < s.rows, row_works = row < s.rows;
+    const int token = row_works ? row / a.group : 0, head = kv_head * a.group + (row_works ? row - token * a.group : 0);
+    const int pos = s.cached + token;
+    float4 qf[D / 16];
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        qf[ks] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row_works)
+            qf[ks] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + (int64_t)(s.start + token) * a.q_stride +
+                                                       (int64_t)head * D + ks * 16 + 4 * quarter);
+    }
+    f32x4 o[D / 16];
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+        o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, lsum = 0.f;
+    bool seen = false;
+
+    const int load_row = tid / PIECES, load_piece = tid % PIECES;
+    float4 kreg[LOADS], vreg[LOADS];
+    int block[LOADS];
+    int there = 0;
+    auto look_up = [&](int step) {
+        const int j0 = keys.tile(step) * kF32Keys;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            block[i] = step < step_end ? table_entry(a, it.seq, j0 + load_row + i * ROWS_PER_LOAD, end) : -1;
+    };
+    auto request = [&](int step) {
+        const int j0 = keys.tile(step) * kF32Keys;
+        there = 0;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = cache_row(a, block[i], kv_head, j0 + load_row + i * ROWS_PER_LOAD);
+            kreg[i] = vreg[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (r >= 0) {
+                const int64_t at = (int64_t)r * D + load_piece * 4;
+                kreg[i] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.k_cache) + at);
+                vreg[i] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.v_cache) + at);
+                there |= 1 << i;
+            }
+        }
+    };
+    if (step_begin < step_end) {
+        look_up(step_begin);
+        request(step_begin);
+        look_up(step_begin + 1);
+    }
+    for (int step = step_begin; step < step_end; ++step) {
+        const int j0 = keys.tile(step) * kF32Keys;
+        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kF32Keys);
+        lds_barrier();  // the tile in front has been read
+        if (tid < kF32Keys)
+            lds_bad[tid] = 0;
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int r = load_row + i * ROWS_PER_LOAD;
+            if (part_seen) {
+                const bool bx = not_finite(vreg[i].x), by = not_finite(vreg[i].y), bz = not_finite(vreg[i].z), bw = not_finite(vreg[i].w);
+                vreg[i] = make_float4(bx ? 0.f : vreg[i].x, by ? 0.f : vreg[i].y, bz ? 0.f : vreg[i].z, bw ? 0.f : vreg[i].w);
+                if (bx || by || bz || bw)
+                    lds_bad[r] = 1;
+            }
+            *reinterpret_cast<float4 *>(kt + r * STRIDE + load_piece * 4) = kreg[i];
+            *reinterpret_cast<float4 *>(vt + r * STRIDE + load_piece * 4) = vreg[i];
+            if (load_piece == 0)
+                flag[r] = there >> i & 1;
+        }
+        if (step + 1 < step_end) {
+            request(step + 1);
+            look_up(step + 2);
+        }
+        lds_barrier();
+        if (!wave_works)
+            continue;
+        f32x4 st[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const float4 kf = *reinterpret_cast<const float4 *>(kt + (kb * 16 + l % 16) * STRIDE + ks * 16 + 4 * quarter);
+                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.x, qf[ks].x, st[kb], 0, 0, 0);
+                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.y, qf[ks].y, st[kb], 0, 0, 0);
+                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.z, qf[ks].z, st[kb], 0, 0, 0);
+                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.w, qf[ks].w, st[kb], 0, 0, 0);
+            }
+        }
+        const uint32_t exist = (uint32_t)__ballot(flag[l % 32] != 0), bad = (uint32_t)__ballot(lds_bad[l % 32] != 0);
+        const bool partly = part_seen || exist != 0xffffffffu;
+        uint32_t hidden = 0;
+        if (partly) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int key = kb * 16 + 4 * quarter + r;
+                    const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos, j0 + key);
+                    hidden |= sees_it ? 0u : 1u << (4 * kb + r);
+                    if (!sees_it)
+                        st[kb][r] = -INFINITY;
+                }
+        }
+        seen = seen || hidden != 0xffu;
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                top = fmaxf(top, st[kb][r]);
+        if (__any(top > m + kOutgrown / a.scale_log2)) {
+            top = fmaxf(top, read_from(top, l ^ 16));
+            top = fmaxf(top, read_from(top, l ^ 32));
+            const float next = fmaxf(m, top), down = next == m ? 1.f : exp2_fast((m - next) * a.scale_log2);
+            m = next;
+            lsum *= down;
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    o[db][r] *= down;
+        }
+        const float mc = finite_max(m) * a.scale_log2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float p = exp2_fast(__builtin_fmaf(st[e / 4][e % 4], a.scale_log2, -mc));
+            if (partly && (hidden >> e & 1))
+                p = 0.f;
+            lsum += p;
+            st[e / 4][e % 4] = p;
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int db = 0; db < D / 16; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(kb * 16 + 4 * quarter + r) * STRIDE + db * 16 + l % 16], st[kb][r], o[db], 0, 0, 0);
+        for (uint32_t left = bad; left != 0; left &= left - 1) {
+            const int key = __builtin_ctz(left), e_of = 4 * (key / 16) + key % 4, from = key % 16 / 4;
+            const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
+            const float *v_row = static_cast<const float *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
+            float p = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                p = e == e_of ? st[e / 4][e % 4] : p;
+            p = read_from(p, l % 16 + 16 * from);
+            const bool sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key);
+#pragma unroll
+            for (int db = 0; db < D / 16; ++db) {
+                const float4 x = *reinterpret_cast<const float4 *>(v_row + db * 16 + 4 * quarter);
+                const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    o[db][e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
+            }
+        }
+    }
+    if (!wave_works)
+        return;
+    lsum += read_from(lsum, l ^ 16);
+    lsum += read_from(lsum, l ^ 32);
+    int any = (int)seen;
+    any |= read_from(any, l ^ 16);
+    any |= read_from(any, l ^ 32);
+    const float w = row_weight(lsum, m, any != 0);
+    if (!row_works)
+        return;
+    const bool split = it.n_splits > 1;
+    const int part = split ? part_of(a, it, kv_head, it.split) : 0;
+    if (split && part >= a.most_parts)
+        return;
+    const int64_t at = (int64_t)part * a.rows_cap + row - r0;
+    const float scale = split ? 1.f : w == 0.f ? 0.f : w < 0.f ? NAN : 1.f / w;
+    float *const dst = split ? a.part + at * D : static_cast<float *>(a.out) + (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D;
+#pragma unroll
+    for (int db = 0; db < D / 16; ++db)
+        *reinterpret_cast<float4 *>(dst + db * 16 + 4 * quarter) =
+            make_float4(o[db][0] * scale, o[db][1] * scale, o[db][2] * scale, o[db][3] * scale);
+    if (quarter == 0) {
+        if (split)
+            *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(m, w);
+        else if (a.lse)
+            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
+    }
+}
+
+// ================================================================ joining
+// The rows of sequences whose keys were split: 16 lanes per row, partial results in their order.
+constexpr int kJoinThreads = 256;
+constexpr int kJoinRows = kJoinThreads / 16;
+
+template <typename E> struct Out {
+    static __device__ __forceinline__ void store4(void *out, int64_t at, const float *v)
+    {
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(E::pack(v[0], v[1]), E::pack(v[2], v[3]));
+    }
+};
+template <> struct Out<float> {
+    static __device__ __forceinline__ void store4(void *out, int64_t at, const float *v)
+    {
+        *reinterpret_cast<float4 *>(static_cast<float *>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+};
+
+template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a)
+{
+    constexpr int BLOCKS = ROWS / kJoinRows;  // workgroups per (tile, key head)
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    const int piece = blockIdx.x % BLOCKS, kv_head = blockIdx.x / BLOCKS % a.Hkv;
+    Item it;
+    if (!find_item<kJoinThreads, ROWS, KT>(a, blockIdx.x / BLOCKS / a.Hkv, true, reinterpret_cast<int *>(lds_raw), &it))
+        return;
+    const Seq s = load_seq(a, it.seq);
+    const int in_tile = piece * kJoinRows + threadIdx.x / 16, row = it.tile * ROWS + in_tile;
+    if (row >= s.rows || part_of(a, it, kv_head, it.n_splits - 1) >= a.most_parts)
+        return;
+    const float *const ml = a.part + (int64_t)a.most_parts * a.rows_cap * D;
+    JoinedRow j;
+    for (int p = 0; p < it.n_splits; ++p)
+        j.add_max(ml[((int64_t)part_of(a, it, kv_head, p) * a.rows_cap + in_tile) * 2]);
+    float v[D / 64][4];
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[i][e] = 0.f;
+    for (int p = 0; p < it.n_splits; ++p) {
+        const int64_t at = (int64_t)part_of(a, it, kv_head, p) * a.rows_cap + in_tile;
+        const float2 x = *reinterpret_cast<const float2 *>(ml + at * 2);
+        const float w = j.add_weight(x.x, x.y, a.scale_log2);
+        if (w != 0.f) {
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const float4 o = *reinterpret_cast<const float4 *>(a.part + at * D + 64 * i + 4 * (threadIdx.x % 16));
+                v[i][0] += w * o.x, v[i][1] += w * o.y, v[i][2] += w * o.z, v[i][3] += w * o.w;
+            }
+        }
+    }
+    const float scale = j.scale();
+    const int token = row / a.group, head = kv_head * a.group + row - token * a.group;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[i][e] *= scale;
+        Out<E>::store4(a.out, (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D + 64 * i + 4 * (threadIdx.x % 16), v[i]);
+    }
+    if (a.lse && threadIdx.x % 16 == 0)
+        a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(j.m, j.weight(), a.scale_log2);
+}
+
+// ---------------------------------------------------------------- choice of kernels
+constexpr int kChunkWaves = 8;
+constexpr int kChunkRows = 32 * kChunkWaves;
+constexpr int kF32Rows = 16 * kF32Waves;
+
+// One launch: which sequences, how many rows per tile, how many workgroups.
+struct Launch {
+    int rows;             // per tile
+    int64_t min_rows, max_rows;
+    uint32_t target;
+    int min_steps;
+    int64_t most_tiles;   // of all sequences, per key head
+    int64_t grid, join_grid, parts, rows_cap;
+    size_t bytes;         // of workspace
+};
+struct Choice {
+    int n;
+    Launch launch[2];
+    bool chunk[2];
+    int row_blocks;       // of the kernel for few rows
+};
+
+Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, int64_t min_rows, int64_t max_rows, uint32_t target, int min_steps)
+{
+    Launch c;
+    const int64_t group = s.n_q_heads / s.n_kv_heads, all_rows = T * group, seqs = batch < T ? batch : T;
+    c.rows = rows;
+    c.min_rows = min_rows;
+    c.max_rows = max_rows;
+    c.target = ATTN_TARGET ? (uint32_t)(ATTN_TARGET) : target;
+    c.min_steps = ATTN_TARGET ? 1 : min_steps;
+    c.most_tiles = max_rows <= rows ? seqs : all_rows / rows + seqs;
+    // A sequence of n steps per tile has ceil(n / per) <= n / per + 1 splits, and the sum of n / per over the tiles is at most
+    // the target.  Only sequences with n > per are split, whose ceil is at most 2 n / per.
+    c.grid = ((c.target + s.n_kv_heads - 1) / s.n_kv_heads + c.most_tiles) * s.n_kv_heads;
+    c.parts = 2 * (int64_t)c.target;
+    c.rows_cap = rows < all_rows ? rows : all_rows;
+    const int64_t split_tiles = c.most_tiles * s.n_kv_heads < c.target ? c.most_tiles * s.n_kv_heads : c.target;
+    c.join_grid = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * (rows / kJoinRows);
+    c.bytes = (size_t)(c.parts * c.rows_cap) * (s.head_dim + 2) * sizeof(float);
+    return c;
+}
+
+Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
+{
+    Choice c;
+    const int64_t group = s.n_q_heads / s.n_kv_heads, most = max_new > 0 && max_new < T ? max_new : T, rows = most * group;
+    const int64_t any = (int64_t)1 << 40;
+    c.n = 1;
+    c.row_blocks = 1;
+    c.chunk[0] = true;
+    if (s.io_dtype == ATTN_DT_F32) {
+        c.launch[0] = make_launch(s, batch, T, kF32Rows, 0, any, 1024, 4);
+        return c;
+    }
+    if (rows <= 64) {
+        c.chunk[0] = false;
+        c.row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        c.launch[0] = make_launch(s, batch, T, 16 * c.row_blocks, 0, any, 1024, 8);
+        return c;
+    }
+    c.launch[0] = make_launch(s, batch, T, kChunkRows, batch > 1 ? 16 : 0, any, 512, 4);
+    if (batch > 1) {
+        c.n = 2;
+        c.chunk[1] = false;
+        c.launch[1] = make_launch(s, batch, T, 16, 0, 16, 1024, 8);
+    }
+    return c;
+}
+
+template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &c, bool few, bool f32, hipStream_t stream)
+{
+    const dim3 grid((unsigned)c.join_grid), block(kJoinThreads);
+    const size_t lds = 16 * sizeof(int);
+    if (f32)
+        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, lds, stream, a);
+    else if (!few)
+        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, lds, stream, a);
+    else if (c.rows == 16)
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, lds, stream, a);
+    else if (c.rows == 32)
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, lds, stream, a);
+    else
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, lds, stream, a);
+    return hipGetLastError();
+}
+
+template <typename K> hipError_t lds_limit(K kernel, size_t lds)
+{
+    return lds > 65536 ? hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)
+                       : hipSuccess;
+}
+
+template <typename E, int D, int RB> hipError_t launch_few(const AttendArgs &a, const Launch &c, hipStream_t stream)
+{
+    constexpr size_t v = (size_t)kFewWaves * FewTile<D>::kBytes, o = (size_t)kFewWaves * 16 * (D + 4 + 2) * sizeof(float);
+    constexpr size_t lds = v > o ? v : o;
+    hipLaunchKernelGGL((attn_few_kernel<E, D, RB>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
+    return hipGetLastError();
+}
+
+template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Launch &c, bool chunk, hipStream_t stream)
+{
+    hipError_t e;
+    if (chunk) {
+        constexpr size_t lds = 4 * (size_t)ChunkTile<D>::kBytes + (2 * kChunkKeys + 2 * kChunkWaves + 8) * sizeof(int);
+        if ((e = lds_limit(attn_chunk_kernel<E, D, kChunkWaves>, lds)) != hipSuccess)
+            return e;
+        hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
+        e = hipGetLastError();
+    } else {
+        e = c.rows == 16 ? launch_few<E, D, 1>(a, c, stream) : c.rows == 32 ? launch_few<E, D, 2>(a, c, stream) : launch_few<E, D, 4>(a, c, stream);
+    }
+    return e != hipSuccess ? e : join<E, D>(a, c, !chunk, false, stream);
+}
+
+template <int D> hipError_t launch_f32(const AttendArgs &a, const Launch &c, hipStream_t stream)
+{
+    constexpr size_t lds = 2 * (size_t)kF32Keys * (D + 4) * sizeof(float) + (2 * kF32Keys + 2 * kF32Waves + 8) * sizeof(int);
+    hipLaunchKernelGGL((attn_f32_kernel<D>), dim3((unsigned)c.grid), dim3(64 * kF32Waves), lds, stream, a);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : join<float, D>(a, c, false, true, stream);
+}
+
+}  // namespace
+
+size_t attn_attend_workspace(const attn_shape_t &s, int batch, int64_t T, int max_new)
+{
+    if (T == 0 || batch == 0)
+        return 0;
+    const Choice c = choose(s, batch, T, max_new);
+    size_t n = 0;
+    for (int i = 0; i < c.n; ++i)
+        n += (c.launch[i].bytes + 255) / 256 * 256;
+    return n;
+}
+
+hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
+                              int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
+                              const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
+                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream)
+{
+    const Choice c = choose(s, batch, T, max_new);
+    for (int i = 0; i < c.n; ++i)
+        if (c.launch[i].grid > 0x7fffffff || c.launch[i].join_grid > 0x7fffffff)
+            return hipErrorInvalidValue;
+    AttendArgs a;
+    a.q = q;
+    a.k_cache = k_cache;
+    a.v_cache = v_cache;
+    a.table = table;
+    a.cu = cu;
+    a.cached = cached;
+    a.out = out;
+    a.lse = lse;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.T = T;
+    a.batch = batch;
+    a.Hq = s.n_q_heads;
+    a.Hkv = s.n_kv_heads;
+    a.group = s.n_q_heads / s.n_kv_heads;
+    a.D = s.head_dim;
+    a.log2_bs = __builtin_ctz((unsigned)s.block_size);
+    a.max_blocks = max_blocks;
+    a.n_blocks = n_blocks;
+    a.window = window;
+    a.sinks = sinks;
+    a.scale_log2 = scale * kLog2e;
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    for (int i = 0; i < c.n; ++i) {
+        const Launch &u = c.launch[i];
+        a.part = reinterpret_cast<float *>(ws);
+        ws += (u.bytes + 255) / 256 * 256;
+        a.min_rows = (int)u.min_rows;
+        a.max_rows = u.max_rows > 0x7fffffff ? 0x7fffffff : (int)u.max_rows;
+        a.rows_cap = (int)u.rows_cap;
+        a.most_parts = (int)u.parts;
+        a.target = u.target;
+        a.min_steps = u.min_steps;
+        hipError_t e;
+        if (s.io_dtype == ATTN_DT_F32)
+            e = s.head_dim == 64 ? launch_f32<64>(a, u, stream) : launch_f32<128>(a, u, stream);
+        else if (s.io_dtype == ATTN_DT_BF16)
+            e = s.head_dim == 64 ? launch16<Bf16, 64>(a, u, c.chunk[i], stream) : launch16<Bf16, 128>(a, u, c.chunk[i], stream);
+        else
+            e = s.head_dim == 64 ? launch16<F16, 64>(a, u, c.chunk[i], stream) : launch16<F16, 128>(a, u, c.chunk[i], stream);
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}

@@ -1,0 +1,319 @@
+// What the attention kernels share (gfx950 only): arguments, how the work of a batch is dealt to workgroups, which keys a
+// query sees, the cache's rows.
+#pragma once
+
+#include "attn_cache.h"
+#include "mfma_utils.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+constexpr int kMaxBatch = 4096;
+
+// ---------------------------------------------------------------- lanes and waves
+__device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
+__device__ __forceinline__ int read_from(int v, int lane) { return __builtin_amdgcn_ds_bpermute(lane << 2, v); }
+__device__ __forceinline__ float read_from(float v, int lane)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(lane << 2, (int)__float_as_uint(v)));
+}
+
+// LDS is ordered, loads in flight stay in flight
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return a + b < a ? 0xffffffffu : a + b; }
+
+// Inclusive prefix sum over the lanes of a wave.
+__device__ __forceinline__ int wave_scan(int v)
+{
+    const int l = lane_id();
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = read_from(v, l >= d ? l - d : l);
+        v += l >= d ? o : 0;
+    }
+    return v;
+}
+
+// ---------------------------------------------------------------- arguments of attn_attend
+struct AttendArgs {
+    const void *q, *k_cache, *v_cache;
+    const int32_t *table, *cu, *cached;
+    void *out;
+    float *lse;
+    float *part;            // partial results: [part][rows_cap][D] sums, then [part][rows_cap][2] maximum and weight
+    int64_t q_stride, out_stride;
+    int64_t T;
+    int32_t batch, Hq, Hkv, group, D;
+    int32_t log2_bs, max_blocks, n_blocks;
+    int32_t window, sinks;
+    float scale_log2;       // scale * log2(e): the softmax runs on powers of two
+    int32_t min_rows, max_rows;  // this launch takes the sequences with min_rows < rows <= max_rows
+    int32_t rows_cap;       // rows of a partial result
+    int32_t most_parts;     // partial results there is room for
+    uint32_t target;        // workgroups that keep the GPU busy
+    int32_t min_steps;      // a workgroup gets no fewer steps of keys than this if it can help it
+};
+
+// ---------------------------------------------------------------- sequences
+struct Seq {
+    int start;   // first packed token
+    int n;       // new tokens
+    int cached;
+    int rows;    // n * group: the row of token i and the group's head h is i * group + h
+};
+__device__ __forceinline__ Seq load_seq(const AttendArgs &a, int b)
+{
+    Seq s;
+    const int64_t from = a.cu[b] < 0 ? 0 : a.cu[b], to = a.cu[b + 1] > a.T ? a.T : a.cu[b + 1];
+    s.start = (int)from;
+    s.n = to > from ? (int)(to - from) : 0;
+    const int64_t most = (int64_t)a.max_blocks << a.log2_bs;  // tokens behind the table's end are not seen
+    const int64_t room = most > 0x3fffffff ? 0x3fffffff : most;
+    const int c = a.cached[b] < 0 ? 0 : a.cached[b];
+    s.cached = c > room ? (int)room : c;
+    s.rows = s.n * a.group;
+    return s;
+}
+
+// Keys that the rows [r0, r0 + ROWS) of a sequence see, in tiles of KT keys: first the sinks' tiles, then [near, end).
+struct KeyRange {
+    int pos0, pos1;  // positions of the first and the last row
+    int near;        // first tile of the window
+    int n_sink;      // tiles of sinks in front of it
+    int n;           // tiles in all
+    __device__ __forceinline__ int tile(int step) const { return step < n_sink ? step : near + step - n_sink; }
+};
+template <int KT> __device__ __forceinline__ KeyRange key_range(const AttendArgs &a, const Seq &s, int r0, int rows)
+{
+    KeyRange k;
+    const int last = r0 + rows < s.rows ? r0 + rows - 1 : s.rows - 1;
+    k.pos0 = s.cached + r0 / a.group;
+    k.pos1 = s.cached + last / a.group;
+    const int lo = a.window > 0 && k.pos0 >= a.window ? k.pos0 - a.window + 1 : 0;
+    k.near = lo / KT;
+    const int sink_tiles = a.sinks / KT + (a.sinks % KT != 0);
+    k.n_sink = sink_tiles < k.near ? sink_tiles : k.near;
+    k.n = k.n_sink + k.pos1 / KT + 1 - k.near;
+    return k;
+}
+// An upper bound of that over the sequence's row tiles.
+template <int KT> __device__ __forceinline__ int most_steps(const AttendArgs &a, const Seq &s, int rows)
+{
+    const int all = (s.cached + s.n - 1) / KT + 1;
+    if (a.window <= 0)
+        return all;
+    const int64_t near = ((int64_t)a.window + rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
+    return near < all ? (int)near : all;
+}
+
+__device__ __forceinline__ bool sees(const AttendArgs &a, int pos, int j)
+{
+    return j <= pos && (a.window <= 0 || pos - j < a.window || j < a.sinks);
+}
+// Every row at positions pos0..pos1 sees every key of [j0, j0 + n).
+__device__ __forceinline__ bool all_see(const AttendArgs &a, int pos0, int pos1, int j0, int n)
+{
+    return j0 + n - 1 <= pos0 && (a.window <= 0 || pos1 - j0 < a.window || j0 + n <= a.sinks);
+}
+
+// ---------------------------------------------------------------- who does what
+// The rows of a sequence are cut into tiles of ROWS rows; the keys of all tiles of a sequence into the same number of
+// splits, as many as it takes to give the GPU `target` workgroups of equal length.  Every workgroup finds its own piece
+// from the lengths: nothing is planned ahead, so the lengths may change between replays of a graph.
+struct Item {
+    int seq, tile, split, n_splits;
+    int part;  // the first partial result of (seq, tile): split s of key head h is part + (tile * n_splits + s) * Hkv + h
+};
+
+// The workgroup's `unit`-th (tile, split), or with `of_join` the unit-th tile of the sequences that are split.  Returns
+// false if there is none.  All threads of the workgroup call it; `lds` has room for 2 * NT / 64 + 8 words.
+template <int NT, int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int unit, bool of_join, int *lds, Item *out)
+{
+    constexpr int W = NT / 64;
+    const int tid = threadIdx.x, wave = tid / 64, l = lane_id();
+    const bool single = a.batch <= NT;
+    Seq mine = {};
+    uint32_t work = 0;  // steps of all workgroups; saturating sums do not depend on their order
+    for (int b = tid; b < a.batch; b += NT) {
+        const Seq s = load_seq(a, b);
+        if (single)
+            mine = s;
+        if (s.rows > a.min_rows && s.rows <= a.max_rows) {
+            const uint64_t w = (uint64_t)((s.rows + ROWS - 1) / ROWS) * (uint64_t)most_steps<KT>(a, s, ROWS) * (uint64_t)a.Hkv;
+            work = sat_add(work, w > 0xffffffffu ? 0xffffffffu : (uint32_t)w);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+        work = sat_add(work, (uint32_t)read_from((int)work, l ^ d));
+    if (l == 0)
+        lds[wave] = (int)work;
+    lds_barrier();
+    work = 0;
+    for (int w = 0; w < W; ++w)
+        work = sat_add(work, (uint32_t)lds[w]);
+    uint32_t per = work / a.target + (work % a.target != 0);  // steps of a workgroup
+    per = per < (uint32_t)a.min_steps ? (uint32_t)a.min_steps : per;
+
+    int items_before = 0, parts_before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += NT) {
+        const int b = b0 + tid;
+        int items = 0, parts = 0, splits = 1;
+        if (b < a.batch) {
+            const Seq s = single ? mine : load_seq(a, b);
+            if (s.rows > a.min_rows && s.rows <= a.max_rows) {
+                const int tiles = (s.rows + ROWS - 1) / ROWS;
+                splits = (int)(((uint32_t)most_steps<KT>(a, s, ROWS) + per - 1) / per);
+                items = tiles * (of_join ? splits > 1 : splits);
+                parts = splits > 1 ? tiles * splits : 0;
+            }
+        }
+        const int items_upto = wave_scan(items), parts_upto = wave_scan(parts);
+        lds_barrier();  // the words of the pass in front have been read
+        if (l == 63) {
+            lds[wave] = items_upto;
+            lds[W + wave] = parts_upto;
+        }
+        if (tid == 0)
+            lds[2 * W] = -1;
+        lds_barrier();
+        int items_all = 0, i0 = items_before, p0 = parts_before;
+        int parts_all = 0;
+        for (int w = 0; w < W; ++w) {
+            if (w < wave) {
+                i0 += lds[w];
+                p0 += lds[W + w];
+            }
+            items_all += lds[w];
+            parts_all += lds[W + w];
+        }
+        const int at = unit - (i0 + items_upto - items);
+        if (at >= 0 && at < items) {
+            lds[2 * W] = b;
+            lds[2 * W + 1] = at;
+            lds[2 * W + 2] = splits;
+            lds[2 * W + 3] = p0 + parts_upto - parts;
+        }
+        lds_barrier();
+        if (lds[2 * W] >= 0) {
+            out->seq = lds[2 * W];
+            out->n_splits = lds[2 * W + 2];
+            const int u = lds[2 * W + 1], per_tile = of_join ? 1 : out->n_splits;
+            out->tile = u / per_tile;
+            out->split = u % per_tile;
+            out->part = lds[2 * W + 3];
+            return true;
+        }
+        items_before += items_all;
+        parts_before += parts_all;
+    }
+    return false;
+}
+__device__ __forceinline__ int part_of(const AttendArgs &a, const Item &it, int kv_head, int split)
+{
+    return (it.part + it.tile * it.n_splits + split) * a.Hkv + kv_head;
+}
+
+// ---------------------------------------------------------------- the cache
+// Row of the key at position j in a cache of [n_blocks * n_kv_heads * block_size] rows, or -1 if the table names no block
+// for it.  The host has checked that rows fit 31 bits; byte offsets take 64.
+__device__ __forceinline__ int cache_row(const AttendArgs &a, int block, int kv_head, int j)
+{
+    if ((uint32_t)block >= (uint32_t)a.n_blocks)
+        return -1;
+    return ((block * a.Hkv + kv_head) << a.log2_bs) + (j & ((1 << a.log2_bs) - 1));
+}
+__device__ __forceinline__ int table_entry(const AttendArgs &a, int seq, int j, int end)
+{
+    const int e = j >> a.log2_bs;
+    return j < end && e < a.max_blocks ? a.table[(int64_t)seq * a.max_blocks + e] : -1;
+}
+
+// ---------------------------------------------------------------- 16-bit types
+struct Bf16 {
+    static constexpr uint32_t kExp = 0x7f80u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack2_bf16(lo, hi); }
+    static __device__ __forceinline__ float lo(uint32_t u) { return bf16_lo(u); }
+    static __device__ __forceinline__ float hi(uint32_t u) { return bf16_hi(u); }
+    static __device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c) { return mfma_bf16(a, b, c); }
+    static __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+struct F16 {
+    static constexpr uint32_t kExp = 0x7c00u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack2_f16(lo, hi); }
+    static __device__ __forceinline__ float lo(uint32_t u) { return f16_lo(u); }
+    static __device__ __forceinline__ float hi(uint32_t u) { return f16_hi(u); }
+    static __device__ __forceinline__ f32x16 mfma32(uint4 a, uint4 b, f32x16 c) { return mfma_f16(a, b, c); }
+    static __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+// Infinities and NaN of two packed values become zeros; true if there were any.
+template <typename E> __device__ __forceinline__ bool drop_not_finite(uint32_t &u)
+{
+    const bool lo = (u & E::kExp) == E::kExp, hi = ((u >> 16) & E::kExp) == E::kExp;
+    u = (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
+    return lo || hi;
+}
+
+__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+
+// Weight of a row's maximum: 0 where nothing finite has been seen yet, so that no infinity is subtracted from itself.
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
+
+// How a row without any weight is marked in a partial result: it saw no key (0), or only scores of minus infinity (-1), of
+// which the softmax is undefined.
+__device__ __forceinline__ float row_weight(float l, float m, bool seen) { return m == -INFINITY && l == 0.f && seen ? -1.f : l; }
+
+// ln of the sum of exponentials of a row whose weights are powers of two of scale_log2 (score - m).
+__device__ __forceinline__ float row_lse(float m, float w, float scale_log2)
+{
+    if (w == 0.f)
+        return -INFINITY;
+    return w < 0.f ? NAN : (m * scale_log2 + __builtin_amdgcn_logf(w)) * 0.69314718055994531f;
+}
+
+// A row put together from partial results (maximum, weight): first every maximum, then every weight.
+struct JoinedRow {
+    float m = -INFINITY, w = 0.f;
+    bool undefined = false;  // a part saw only scores of minus infinity
+    __device__ __forceinline__ void add_max(float part_m) { m = fmaxf(m, part_m); }
+    // the factor of the part's sums; 0 if the part has none
+    __device__ __forceinline__ float add_weight(float part_m, float part_w, float scale_log2)
+    {
+        undefined = undefined || part_w < 0.f;
+        if (part_w == 0.f || part_w < 0.f)
+            return 0.f;
+        // a part without a maximum and with weight has seen a NaN and nothing larger than minus infinity
+        const float f = part_m == m ? 1.f : exp2_fast((finite_max(part_m) - m) * scale_log2);
+        w += part_w * f;
+        return f;
+    }
+    __device__ __forceinline__ float weight() const { return w == 0.f && undefined ? -1.f : w; }
+    __device__ __forceinline__ float scale() const { return w == 0.f ? (undefined ? NAN : 0.f) : 1.f / w; }
+};
+
+}  // namespace
+
+// Launchers implemented next to their kernels.
+hipError_t launch_attn_assign(int batch, int log2_bs, int max_blocks, int64_t T, const int32_t *cu, const int32_t *cached,
+                              const int32_t *shared, const int32_t *table_in, int32_t *table_out, const int32_t *free_blocks,
+                              const int32_t *n_free, int32_t free_capacity, int64_t *slots, int32_t *positions, int32_t *copies,
+                              int32_t *counts, hipStream_t stream);
+hipError_t launch_attn_rope(const attn_shape_t &s, int64_t T, int batch, int n_blocks, const void *q, int64_t q_stride,
+                            const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *positions,
+                            const int64_t *slots, const float *rotary, int max_positions, int rotary_dim, bool interleaved,
+                            const int32_t *copies, void *q_out, void *k_cache, void *v_cache, hipStream_t stream);
+hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
+                              int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
+                              const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
+                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream);
+size_t attn_attend_workspace(const attn_shape_t &s, int batch, int64_t T, int max_new);

@@ -1,0 +1,242 @@
+"""The attention operators on the GPU, through the Python entry points, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import attn_helpers as ah
+import attn_oracle
+from test_attention_emulation import ASSIGN, CASES, NOT_FINITE, ROPE, rope_check, rope_problem
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def _attend(p, **kw):
+    from paper_2411_19379_amd import attention as attn
+    out, lse = attn.attend(p.q.to(DEV), p.k_cache.to(DEV), p.v_cache.to(DEV), _dev(p.table), _dev(p.cu), _dev(np.array(p.cached, np.int32)),
+                           scale=p.scale, window=p.window, sinks=p.sinks, max_new=p.max_new, return_lse=True, **kw)
+    return out.double().cpu().numpy(), lse.cpu().numpy()
+
+
+@pytest.mark.parametrize("name", sorted(CASES))
+def test_attend_small(name):
+    print(f"attend {name}", flush=True)
+    p = ah.make(11, *CASES[name])
+    ah.check(p, *_attend(p), name)
+
+
+@pytest.mark.parametrize("name", ["decode", "few_window", "chunk", "chunk_window", "f32_wide_window"])
+def test_attend_with_blocks_missing(name):
+    print(f"attend holes {name}", flush=True)
+    p = ah.make(5, *CASES[name], holes=0.5)
+    ah.check(p, *_attend(p), name)
+
+
+@pytest.mark.parametrize("where", ["v", "k"])
+@pytest.mark.parametrize("name", NOT_FINITE)
+def test_attend_not_finite(name, where):
+    print(f"attend not finite {name} {where}", flush=True)
+    p = ah.make(7, *CASES[name])
+    cache = p.v_cache if where == "v" else p.k_cache
+    for i, bad in enumerate([float("inf"), float("nan"), -float("inf")]):
+        seq = max(range(len(p.new)), key=lambda b: p.new[b])
+        total = p.new[seq] + p.cached[seq]
+        for j in {total - 1 - 2 * i, total // 2 + i, total * 3 // 4 - i}:
+            if 0 <= j < total:
+                block, row = p.block_row(seq, j)
+                cache[block, i % p.hkv, row, (5 * i + j) % p.d] = bad
+    ah.check(p, *_attend(p), name)
+
+
+def _reference64(p):
+    """The definition with torch in 64 bits on the GPU, for lengths the plain oracle takes too long for."""
+    T, hq, d, g = p.T, p.hq, p.d, p.hq // p.hkv
+    out = torch.zeros((T, hq, d), dtype=torch.float64, device=DEV)
+    size = torch.zeros_like(out)
+    lse = torch.full((T, hq), -float("inf"), dtype=torch.float64, device=DEV)
+    for b in range(len(p.new)):
+        n, c = p.new[b], p.cached[b]
+        if n == 0:
+            continue
+        j = torch.arange(n + c, device=DEV)
+        blocks = _dev(p.table[b]).long()[j // p.bs]
+        there = (blocks >= 0) & (blocks < p.k_cache.shape[0])
+        blocks = blocks.clamp(0, p.k_cache.shape[0] - 1)
+        k = p.k_cache.to(DEV)[blocks, :, j % p.bs].double()
+        v = p.v_cache.to(DEV)[blocks, :, j % p.bs].double()
+        k[~there] = 0
+        v[~there] = 0
+        pos = torch.arange(c, c + n, device=DEV)[:, None]
+        seen = (j <= pos) & there
+        if p.window:
+            seen &= (j > pos - p.window) | (j < p.sinks)
+        for h in range(hq):
+            s = p.q[p.cu[b]:p.cu[b + 1], h].to(DEV).double() @ k[:, h // g].T * p.scale
+            s[~seen] = -float("inf")
+            some = seen.any(1)
+            w = torch.softmax(s, 1)
+            w[~some] = 0
+            rows = slice(int(p.cu[b]), int(p.cu[b + 1]))
+            out[rows, h] = w @ v[:, h // g]
+            size[rows, h] = w @ v[:, h // g].abs()
+            lse[rows, h] = torch.logsumexp(s, 1)
+    return out.cpu().numpy(), lse.cpu().numpy(), size.cpu().numpy()
+
+
+# heads, key heads, head_dim, block size, type, new tokens, cached tokens, window, sinks, max_new
+LONG = {
+    "decode_long": (8, 2, 128, 16, "bf16", [1] * 5, [9000, 1, 4096, 333, 20000], 0, 0, 1),
+    "decode_long_f16_window": (8, 8, 64, 32, "f16", [1] * 4, [9000, 1, 4097, 333], 1000, 4, 1),
+    "speculative": (8, 2, 128, 64, "bf16", [5, 3, 1, 8], [5000, 17, 4096, 333], 0, 0, 8),
+    "speculative_wide": (32, 2, 64, 16, "f16", [4, 2], [3000, 170], 0, 0, 4),
+    "chunk_over_long": (4, 1, 128, 16, "bf16", [137], [6000], 0, 0, 137),
+    "mixed": (8, 2, 128, 16, "f16", [1, 300, 1, 0, 77, 2], [2000, 100, 1, 5, 1500, 64], 0, 0, 0),
+    "mixed_window": (6, 2, 64, 8, "bf16", [1, 300, 1, 0, 777, 2], [2000, 100, 1, 5, 1500, 64], 200, 70, 0),
+    "prompt": (4, 2, 128, 32, "bf16", [2100], [0], 0, 0, 0),
+    "prompt_f16_small_heads": (6, 3, 64, 16, "f16", [1500, 900], [64, 63], 0, 0, 0),
+    "f32_long": (4, 2, 128, 16, "f32", [1, 200], [5000, 700], 0, 0, 0),
+}
+
+
+@pytest.mark.parametrize("name", sorted(LONG))
+def test_attend_long(name):
+    print(f"attend {name}", flush=True)
+    p = ah.make(21, *LONG[name])
+    ah.check(p, *_attend(p), name, ref=_reference64(p))
+
+
+def test_attend_rows_of_a_projection_on_another_stream():
+    """q is a part of wider rows, out as well; the call goes to the stream that is current."""
+    from paper_2411_19379_amd import attention as attn
+    p = ah.make(4, *LONG["mixed"])
+    wide = torch.full((p.T, p.hq + 3, p.d), float("nan"), dtype=p.q.dtype, device=DEV)
+    wide[:, 2:2 + p.hq] = p.q.to(DEV)
+    out_wide = torch.full_like(wide, 7.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        q = wide[:, 2:2 + p.hq] * 1  # made on that stream
+        wide[:, 2:2 + p.hq].copy_(q)
+        out, lse = attn.attend(wide[:, 2:2 + p.hq], p.k_cache.to(DEV), p.v_cache.to(DEV), _dev(p.table), _dev(p.cu),
+                               _dev(np.array(p.cached, np.int32)), scale=p.scale, out=out_wide[:, 1:1 + p.hq], return_lse=True)
+    side.synchronize()
+    ah.check(p, out.double().cpu().numpy(), lse.cpu().numpy(), ref=_reference64(p))
+    assert bool((out_wide[:, 0] == 7.0).all()) and bool((out_wide[:, 1 + p.hq:] == 7.0).all())
+
+
+def test_attend_offsets_beyond_32_bits():
+    """Blocks whose byte offsets in the cache pass 2^32."""
+    from paper_2411_19379_amd import attention as attn
+    hkv, bs, d = 8, 64, 128
+    n_blocks = (5 << 30) // (hkv * bs * d * 2)
+    new, cached = [1, 100], [300, 150]
+    p = ah.make(6, 16, hkv, d, bs, "bf16", new, cached, max_new=0)
+    k = torch.full((n_blocks, hkv, bs, d), float("nan"), dtype=torch.bfloat16, device=DEV)
+    v = torch.full_like(k, float("nan"))
+    far = {int(b): n_blocks - 1 - i * 3 for i, b in enumerate(sorted(set(p.table[p.table >= 0].tolist())))}
+    table = p.table.copy()
+    for b, to in far.items():
+        k[to], v[to] = p.k_cache[b].to(DEV), p.v_cache[b].to(DEV)
+        table[p.table == b] = to
+    for max_new in (0, 1):
+        out, lse = attn.attend(p.q.to(DEV), k, v, _dev(table), _dev(p.cu), _dev(np.array(cached, np.int32)), scale=p.scale,
+                               max_new=max_new, return_lse=True)
+        ah.check(p, out.double().cpu().numpy(), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("name", sorted(ASSIGN))
+def test_assign(name, in_place):
+    from paper_2411_19379_amd import attention as attn
+    print(f"assign {name}", flush=True)
+    bs, new, cached, forks, n_free = ASSIGN[name]
+    rs = np.random.RandomState(1)
+    batch, cu = len(new), np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    width = max(-(-(n + c) // bs) for n, c in zip(new, cached)) + 2
+    ids = rs.permutation(batch * width + n_free + 3).astype(np.int32)
+    table = np.full((batch, width), -1, np.int32)
+    for b, c in enumerate(cached):
+        table[b, :-(-c // bs)] = ids[b * width:b * width - (-c // bs)]
+    free = np.concatenate([ids[batch * width:batch * width + n_free], [-5, -5]]).astype(np.int32)
+    shared = rs.randint(0, 2, batch).astype(np.int32) if forks else None
+    want = attn_oracle.assign(bs, cu, cached, table, free, n_free, shared)
+    step = attn.assign_blocks(bs, int(cu[-1]), _dev(cu), _dev(np.array(cached, np.int32)), _dev(table), _dev(free),
+                              _dev(np.array([n_free], np.int32)), shared_tail=None if shared is None else _dev(shared), in_place=in_place)
+    for g, w, what in zip(step, want, ("table", "slots", "positions", "copies", "counts")):
+        assert np.array_equal(g.cpu().numpy(), w), f"{name}: {what}"
+
+
+@pytest.mark.parametrize("name", sorted(ROPE))
+def test_rope_append(name):
+    from paper_2411_19379_amd import attention as attn
+    print(f"rope {name}", flush=True)
+    hq, hkv, d, bs, dtype, rot, inter, T = ROPE[name]
+    problem = rope_problem(name)
+    qkv, caches, rotary, positions, slots, copies = problem
+    x, k_cache, v_cache = qkv.to(DEV), caches[0].to(DEV), caches[1].to(DEV)
+    q_out = attn.rope_append(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], _dev(positions), _dev(slots),
+                             rotary.to(DEV) if rot else None, k_cache, v_cache, interleaved=bool(inter), copies=_dev(copies))
+    rope_check(name, problem, q_out.cpu(), k_cache.cpu(), v_cache.cpu())
+    q = x[:, :hq].contiguous()
+    same = attn.rope_append(q, x[:, hq:hq + hkv], x[:, hq + hkv:], _dev(positions), _dev(slots),
+                            rotary.to(DEV) if rot else None, k_cache, v_cache, interleaved=bool(inter), q_out=q)
+    assert same.data_ptr() == q.data_ptr() and torch.equal(q.cpu().view(torch.uint8), q_out.cpu().view(torch.uint8))
+
+
+def test_a_captured_step_follows_the_lengths():
+    """Assign, append and attend captured once and replayed while the lengths on the GPU grow: every replay equals the eager
+    calls, with other work and synchronisations between the replays."""
+    from paper_2411_19379_amd import attention as attn
+    hq, hkv, d, bs, batch = 8, 2, 128, 16, 3
+    g = torch.Generator().manual_seed(1)
+    n_blocks, width = 64, 16
+    cached = torch.tensor([30, 1, 47], dtype=torch.int32, device=DEV)
+    cu = torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    free = torch.randperm(n_blocks, generator=g).to(torch.int32).to(DEV)
+    rotary = attn.rotary_table(width * bs, d)
+    qkv = torch.randn((batch, hq + 2 * hkv, d), generator=g).to(torch.bfloat16).to(DEV)
+
+    def start():
+        table = torch.full((batch, width), -1, dtype=torch.int32, device=DEV)
+        table[0, :2], table[1, :1], table[2, :3] = free[:2], free[2:3], free[3:6]
+        gg = torch.Generator().manual_seed(2)
+        caches = [torch.randn((n_blocks, hkv, bs, d), generator=gg).to(torch.bfloat16).to(DEV) for _ in range(2)]
+        return table, free[6:].contiguous(), torch.tensor([n_blocks - 6], dtype=torch.int32, device=DEV), caches
+
+    def step(x, lens, table, pool, n_free, caches):
+        s = attn.assign_blocks(bs, batch, cu, lens, table, pool, n_free, in_place=True)
+        q = attn.rope_append(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], s.positions, s.slots, rotary, *caches)
+        out = attn.attend(q, *caches, s.table, cu, lens, max_new=1)
+        n_free.copy_(s.counts[:1])
+        lens += 1
+        return out
+
+    xs = [torch.randn_like(qkv) for _ in range(20)]
+    table, pool, n_free, caches = start()
+    lens = cached.clone()
+    eager = [step(x, lens, table, pool, n_free, caches).clone() for x in xs]
+
+    table, pool, n_free, caches = start()
+    lens, x_in = cached.clone(), qkv.clone()
+    keep = [t.clone() for t in (table, n_free, *caches, lens)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x_in, lens, table, pool, n_free, caches)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x_in, lens, table, pool, n_free, caches)
+    for t, k in zip((table, n_free, *caches, lens), keep):
+        t.copy_(k)
+    for i, x in enumerate(xs):
+        x_in.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[i]), f"replay {i}"
+        attn.attend(xs[0][:, :hq].contiguous(), *caches, table, cu, cached)  # eager work between the replays
+    assert lens.tolist() == [50, 21, 67]
