@@ -27,32 +27,47 @@ template <typename E> __device__ __forceinline__ void unpack4(uint2 u, float *v)
 }
 
 // ================================================================ chunks
-// A workgroup takes 32 rows per wave and walks the keys in tiles of 64, K and V in LDS in two buffers: while a tile is worked
-// on, the next one is on its way in registers.
+// A workgroup takes 32 rows per wave and walks the keys in tiles of 64, K and V in LDS in three buffers each.
+//
+// A wave alternates between products, O += V^T(t-1) P^T(t-1) and S = K(t) Q^T, and the softmax of tile t on the vector ALUs;
+// a tile costs about the same in both.  The two waves of a SIMD are kept one such phase apart by the workgroup's barriers, so
+// that one's products run under the other's softmax: side by side in the same phase the two kinds of work took turns.
+//
+// With phases numbered from 0, the first half of the waves does products t in phase 2t and softmax t in phase 2t + 1, the other
+// half one phase later.  V(t + 1) and K(t + 2) are requested at the start of a wave's softmax t, phase 2t + 1 or 2t + 2, behind
+// the last reads of what they replace, V(t - 2) and K(t - 1) in phase 2t - 1; a wave waits for what it has requested at the end
+// of its products t + 1, phase 2t + 2 or 2t + 3, and the first reads are in phase 2t + 4.
 constexpr int kChunkKeys = 64;
+
+constexpr int kChunkBuffers = 3;
 
 template <int D> struct ChunkTile {
     static constexpr int kPieces = D / 8;  // 16-byte pieces of a row
     static constexpr int kBytes = kChunkKeys * D * 2;
-    // Where piece c of row r lies.  K is read 32 rows at a piece, V 8 rows at four neighbouring pieces: both without two lanes
-    // of a group on one bank.
-    static __device__ __forceinline__ int k_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) << 4); }
-    static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2)) << 4); }
+    // Piece c of row r lies at piece c ^ turn(r) of the row.  K is read 32 rows at a piece, V 8 rows at four neighbouring pieces:
+    // both without two lanes of a group on one bank.
+    static __device__ __forceinline__ int k_turn(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+    static __device__ __forceinline__ int v_turn(int r) { return D == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
+    static __device__ __forceinline__ int k_at(int r, int c) { return r * D * 2 + ((c ^ k_turn(r)) << 4); }
+    static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ v_turn(r)) << 4); }
 };
 
-template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) void attn_chunk_kernel(AttendArgs a)
+template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 * NW, 2) void attn_chunk_kernel(AttendArgs a)
 {
     typedef ChunkTile<D> Tile;
     constexpr int NT = 64 * NW, ROWS = 32 * NW, PIECES = Tile::kPieces;
-    constexpr int LOADS = kChunkKeys * PIECES / NT;  // pieces of K (and of V) per thread and tile
-    constexpr int ROWS_PER_LOAD = NT / PIECES;
-    static_assert(LOADS * NT == kChunkKeys * PIECES && PIECES <= 64, "whole tiles");
+    constexpr int KEYS = kChunkKeys / NW;        // of a tile, that a wave moves
+    constexpr int LOADS = KEYS * PIECES / 64;    // copies of K (and of V) for them
+    constexpr int ROWS_PER_LOAD = 64 / PIECES;
+    static_assert(LOADS * ROWS_PER_LOAD == KEYS && KEYS == 8 && NW % 2 == 0, "whole tiles; KEYS is also the smallest wide block");
     extern __shared__ __align__(16) unsigned char lds_raw[];
-    unsigned char *const lds_k = lds_raw, *const lds_v = lds_raw + 2 * Tile::kBytes;
-    int *const lds_flag = reinterpret_cast<int *>(lds_raw + 4 * Tile::kBytes);  // [2][64]: bit 0 the key exists, bit 1 its V is not finite
-    int *const lds_item = lds_flag + 2 * kChunkKeys;
+    unsigned char *const lds_k = lds_raw, *const lds_v = lds_raw + kChunkBuffers * Tile::kBytes;
+    // of four tiles: which keys exist, and whose V is not finite
+    int *const lds_exist = reinterpret_cast<int *>(lds_raw + 2 * kChunkBuffers * Tile::kBytes), *const lds_bad = lds_exist + 4 * kChunkKeys;
+    int *const lds_item = lds_bad + 4 * kChunkKeys;
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), half = l / 32;
+    const bool late = wave >= NW / 2;  // one phase behind the others
     const int kv_head = blockIdx.x % a.Hkv;
     Item it;
     if (!find_item<NT, ROWS, kChunkKeys>(a, blockIdx.x / a.Hkv, false, lds_item, &it))
@@ -60,7 +75,8 @@ template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) vo
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
     const KeyRange keys = key_range<kChunkKeys>(a, s, r0, ROWS);
-    const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
+    const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits);
+    const int n = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits) - step_begin;
     const int end = keys.pos1 + 1;  // no row of the workgroup sees a key behind it
 
     // this lane's row
@@ -80,100 +96,187 @@ template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) vo
                                                       (int64_t)head * D + ks * 16 + 8 * half);
     }
 
-    f32x16 o[D / 32];
+    f32x16 o[D / 32], st[2];
+    uint4 pf[4];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
         o[db] = zero16();
     float m = -INFINITY, lsum = 0.f;
     bool seen = false;
+    const float outgrown = kOutgrown / a.scale_log2;
 
-    // what this thread loads: rows load_row + i * ROWS_PER_LOAD, piece load_piece
-    const int load_row = tid / PIECES, load_piece = tid % PIECES;
-    uint4 kreg[LOADS], vreg[LOADS];
-    int block[LOADS];
-    int there = 0;  // bit i: the key exists
-    auto look_up = [&](int step) {  // the blocks of a tile's rows
-        const int j0 = keys.tile(step) * kChunkKeys;
+    // What this wave moves: KEYS neighbouring keys, of V of one tile and of K of the next; this lane piece load_at of its rows,
+    // from where that piece of the row is.  With WIDE, blocks of at least KEYS keys, they lie in one block: one scalar look-up,
+    // uniform addresses (32768 tokens over 16384 cached: 16.4 ms, with a look-up and an address per lane 18.6).  A key that does
+    // not exist is read from the cache's first rows, so that no load waits for a branch: what it gets as K comes to nothing in
+    // the softmax, as V it is cleared.
+    const int load_row = wave * KEYS + l / PIECES, load_at = l % PIECES;
+    const SeenTiles seen_by_all(a, keys.pos0, keys.pos1, kChunkKeys), seen_by_wave(a, wave_pos0, wave_pos1, kChunkKeys);
+    const int32_t *const table = reinterpret_cast<const int32_t *>(own_pointer(a.table + (int64_t)it.seq * a.max_blocks));
+    const unsigned char *const k_cache = own_pointer(a.k_cache), *const v_cache = own_pointer(a.v_cache);
+    const int bs_mask = (1 << a.log2_bs) - 1;
+    const uint32_t lds_k_wave = lds_address(lds_k) + wave * KEYS * D * 2, lds_v_wave = lds_address(lds_v) + wave * KEYS * D * 2;
+    uint32_t k_offset[LOADS], v_offset[LOADS];  // bytes behind the wave's first key's row
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            block[i] = step < step_end ? table_entry(a, it.seq, j0 + load_row + i * ROWS_PER_LOAD, end) : -1;
-    };
-    auto request = [&](int step) {
-        const int j0 = keys.tile(step) * kChunkKeys;
-        there = 0;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int r = cache_row(a, block[i], kv_head, j0 + load_row + i * ROWS_PER_LOAD);
-            kreg[i] = vreg[i] = make_uint4(0, 0, 0, 0);
-            if (r >= 0) {
-                const int64_t at = (int64_t)r * D + load_piece * 8;
-                kreg[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.k_cache) + at);
-                vreg[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.v_cache) + at);
-                there |= 1 << i;
-            }
-        }
-    };
-
-    if (step_begin < step_end) {
-        look_up(step_begin);
-        request(step_begin);
-        look_up(step_begin + 1);
+    for (int i = 0; i < LOADS; ++i) {
+        const int r = load_row + i * ROWS_PER_LOAD;
+        k_offset[i] = (r - wave * KEYS) * D * 2 + ((load_at ^ Tile::k_turn(r)) << 4);
+        v_offset[i] = (r - wave * KEYS) * D * 2 + ((load_at ^ Tile::v_turn(r)) << 4);
     }
-    for (int step = step_begin; step < step_end; ++step) {
-        const int buf = step & 1, j0 = keys.tile(step) * kChunkKeys;
-        unsigned char *const kt = lds_k + buf * Tile::kBytes, *const vt = lds_v + buf * Tile::kBytes;
-        int *const flag = lds_flag + buf * kChunkKeys;
-        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kChunkKeys);  // by the workgroup
+    constexpr int LOOKS = WIDE ? 1 : LOADS;
+    int block[LOOKS], k_row[LOOKS], v_row[LOOKS];  // WIDE: of the wave's first key, else of the lane's
+#pragma unroll
+    for (int i = 0; i < LOOKS; ++i)
+        k_row[i] = -1;
+    auto first_key = [&](int t) __attribute__((always_inline)) { return keys.tile(step_begin + t) * kChunkKeys; };
+    auto look_up = [&](int j0) __attribute__((always_inline)) {  // the blocks of a tile's keys
+#pragma unroll
+        for (int i = 0; i < LOOKS; ++i) {
+            const int e = (j0 + (WIDE ? wave * KEYS : load_row + i * ROWS_PER_LOAD)) >> a.log2_bs;
+            const int at = (uint32_t)e < (uint32_t)a.max_blocks ? e : a.max_blocks - 1;
+            block[i] = WIDE ? scalar_load(table + at) : table[at];
+        }
+    };
+    // V of a tile, K of tile t behind it, whose first key is j0 and whose blocks have been looked up
+    auto request = [&](int v_buf, int j0, int t, int k_buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LOOKS; ++i) {
+            const int j = j0 + (WIDE ? wave * KEYS : load_row + i * ROWS_PER_LOAD);
+            v_row[i] = k_row[i];
+            k_row[i] = j < end && (uint32_t)block[i] < (uint32_t)a.n_blocks ? ((block[i] * a.Hkv + kv_head) << a.log2_bs) + (j & bs_mask) : -1;
+            // WIDE: one word for the wave's keys, else one for each; the same from all lanes of it
+            lds_exist[(t & 3) * kChunkKeys + (WIDE ? wave * KEYS : load_row + i * ROWS_PER_LOAD)] = k_row[i] >= 0;
+        }
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int r = load_row + i * ROWS_PER_LOAD;
-            bool bad = false;
-            if (part_seen) {
-                bad = drop_not_finite<E>(vreg[i].x) || bad;
-                bad = drop_not_finite<E>(vreg[i].y) || bad;
-                bad = drop_not_finite<E>(vreg[i].z) || bad;
-                bad = drop_not_finite<E>(vreg[i].w) || bad;
-            }
-            const uint64_t any = __ballot(bad);
-            const uint64_t of_row = any >> (l / PIECES * PIECES) & ((1ull << (PIECES - 1) << 1) - 1);
-            *reinterpret_cast<uint4 *>(kt + Tile::k_at(r, load_piece)) = kreg[i];
-            *reinterpret_cast<uint4 *>(vt + Tile::v_at(r, load_piece)) = vreg[i];
-            if (load_piece == 0)
-                flag[r] = (there >> i & 1) | (of_row != 0 ? 2 : 0);
-        }
-        if (step + 1 < step_end) {
-            request(step + 1);
-            look_up(step + 2);
-        }
-        lds_barrier();
-        if (!wave_works)
-            continue;
-
-        f32x16 st[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            st[kb] = zero16();
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const uint4 kf = *reinterpret_cast<const uint4 *>(kt + Tile::k_at(kb * 32 + l % 32, 2 * ks + half));
-                st[kb] = E::mfma32(kf, qf[ks], st[kb]);
+            const uint32_t to_v = lds_v_wave + v_buf * Tile::kBytes + i * ROWS_PER_LOAD * D * 2, to_k = lds_k_wave + k_buf * Tile::kBytes + i * ROWS_PER_LOAD * D * 2;
+            const int vr = v_row[WIDE ? 0 : i], kr = k_row[WIDE ? 0 : i];
+            const unsigned char *const v = v_cache + (uint64_t)(uint32_t)(vr < 0 ? 0 : vr) * (D * 2), *const k = k_cache + (uint64_t)(uint32_t)(kr < 0 ? 0 : kr) * (D * 2);
+            if (WIDE) {
+                copy16_to_lds(v, v_offset[i], to_v);
+                copy16_to_lds(k, k_offset[i], to_k);
+            } else {
+                const int own = (l / PIECES + i * ROWS_PER_LOAD) * D * 2;
+                copy16_to_lds(v + v_offset[i] - own, to_v);
+                copy16_to_lds(k + k_offset[i] - own, to_k);
             }
         }
-        const int f = flag[l];
-        const uint64_t exist = __ballot((f & 1) != 0), bad = __ballot((f & 2) != 0);
-        const bool partly = !all_see(a, wave_pos0, wave_pos1, j0, kChunkKeys) || exist != ~0ull;
-        uint32_t hidden = 0;  // bit 16 kb + r: the row does not see that key
-        if (partly) {
+    };
+    auto arrive = [&](int t, int j0, int v_buf) __attribute__((always_inline)) {  // what the last request asked for, V of tile t
+        memory_wait();
+        const bool part_seen = !seen_by_all.all(j0);
+        bool missing = WIDE && j0 + kChunkKeys > end;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i < LOOKS; ++i)
+            missing = missing || v_row[i] < 0;
+        if (part_seen || __any(missing)) {
+            const int l = unknown(lane_id()), load_at = l % PIECES;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = kb * 32 + 8 * (r / 4) + 4 * half + r % 4;
-                    const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos, j0 + key);
-                    hidden |= sees_it ? 0u : 1u << (16 * kb + r);
-                    if (!sees_it)
-                        st[kb][r] = -INFINITY;
+            for (int i = 0; i < LOADS; ++i) {
+                const int r = wave * KEYS + l / PIECES + i * ROWS_PER_LOAD;
+                uint4 *const at = reinterpret_cast<uint4 *>(lds_v + v_buf * Tile::kBytes + r * D * 2 + load_at * 16);
+                uint4 v = v_row[WIDE ? 0 : i] < 0 || j0 + r >= end ? make_uint4(0, 0, 0, 0) : *at;
+                if (part_seen) {
+                    bool bad = drop_not_finite<E>(v.x);
+                    bad = drop_not_finite<E>(v.y) || bad;
+                    bad = drop_not_finite<E>(v.z) || bad;
+                    bad = drop_not_finite<E>(v.w) || bad;
+                    const uint64_t of_row = __ballot(bad) >> (l / PIECES * PIECES) & ((1ull << (PIECES - 1) << 1) - 1);
+                    lds_bad[(t & 3) * kChunkKeys + r] = of_row != 0;
                 }
+                *at = v;
+            }
+        }
+    };
+    // The operands' reads run kAhead products ahead of their use, through both products of a phase.  With the buffers known at
+    // compile time their addresses differ by constants: 4 for V (2 with 64 values per head) and 8 (4) for K.
+    constexpr int PV = 4 * (D / 32), QK = 2 * (D / 16), kAhead = 6;
+    int v_base[D / 32], k_base[D / 16];
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+        v_base[db] = kChunkBuffers * Tile::kBytes + Tile::v_at(4 * half + l % 16 / 4, db * 4 + 2 * (l / 16 % 2) + l % 4 / 2) + 8 * (l % 2);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+        k_base[ks] = Tile::k_at(l % 32, 2 * ks + half);
+    auto values = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < PV; ++i) {
+            const unsigned char *const p = lds_raw + v_base[i % (D / 32)] + buf * Tile::kBytes + i / (D / 32) * 16 * D * 2;
+            o[i % (D / 32)] = E::mfma32(lds_frag_tr(p, p + 8 * D * 2), pf[i / (D / 32)], o[i % (D / 32)]);
+        }
+    };
+    auto scores = [&](int buf) __attribute__((always_inline)) {
+        st[0] = st[1] = zero16();
+#pragma unroll
+        for (int i = 0; i < QK; ++i) {
+            const uint4 k = *reinterpret_cast<const uint4 *>(lds_raw + k_base[i % (D / 16)] + buf * Tile::kBytes + i / (D / 16) * 32 * D * 2);
+            st[i / (D / 16)] = E::mfma32(k, qf[i % (D / 16)], st[i / (D / 16)]);
+        }
+    };
+    auto products = [&](int v_buf, int k_buf) __attribute__((always_inline)) {
+        constexpr int kDsRead = 0x100, kMfma = 0x8;
+        values(v_buf);
+        scores(k_buf);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2 * kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < PV; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+            if (i + kAhead < PV)
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+            else
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < QK; ++i) {
+            __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+            if (i + kAhead < QK)
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        }
+    };
+    auto not_finite_values = [&](int t, int j0) __attribute__((always_inline)) {
+        if (seen_by_all.all(j0))
+            return;
+        const int l = unknown(lane_id()), half = l / 32;
+        const uint64_t bad = __ballot(lds_bad[(t & 3) * kChunkKeys + l] != 0);
+        for (uint64_t left = bad; left != 0; left &= left - 1) {
+            // V of this key has infinities or NaN, which are zeros in LDS: they go to the rows that see the key
+            const int key = __builtin_ctzll(left), word = 8 * (key / 32) + 2 * (key % 32 / 8) + key % 4 / 2, from = key % 8 / 4;
+            uint32_t two = 0;
+#pragma unroll
+            for (int w = 0; w < 16; ++w) {
+                const uint4 f = pf[w / 4];
+                two = w == word ? (w % 4 == 0 ? f.x : w % 4 == 1 ? f.y : w % 4 == 2 ? f.z : f.w) : two;
+            }
+            const float p = read_from(key % 2 ? E::hi(two) : E::lo(two), l % 32 + 32 * from);
+            const int j = j0 + key, cr = cache_row(a, table_entry(a, it.seq, j, end), kv_head, j);
+            const uint32_t sees_it = row_works && cr >= 0 && sees(a, pos, j) ? ~0u : 0u;
+            const uint16_t *v_of = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+                    unpack4<E>(*reinterpret_cast<const uint2 *>(v_of + db * 32 + 8 * q + 4 * half), v);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[db][4 * q + e] += not_finite_part(p, v[e], sees_it);
+                }
+        }
+    };
+    auto softmax = [&](int t, int j0) __attribute__((always_inline)) {
+        const uint64_t exist = __ballot(lds_exist[(t & 3) * kChunkKeys + (WIDE ? l & -KEYS : l)] != 0);
+        if (!seen_by_wave.all(j0) || exist != ~0ull) {
+            const uint64_t keys_seen = seen_keys(a, unknown(pos), j0, exist);
+            seen = seen || keys_seen != 0;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const uint32_t mine = (uint32_t)(keys_seen >> (32 * kb)) >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    st[kb][r] = seen_score(st[kb][r], mine, 8 * (r / 4) + r % 4);
+            }
+        } else {
+            seen = true;
         }
         float top = -INFINITY;
 #pragma unroll
@@ -181,8 +284,7 @@ template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) vo
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 top = fmaxf(top, st[kb][r]);
-        seen = seen || hidden != 0xffffffffu;
-        if (__any(top > m + kOutgrown / a.scale_log2)) {
+        if (__any(top > m + outgrown)) {
             const float both = fmaxf(top, read_from(top, l ^ 32)), next = fmaxf(m, both);
             const float down = next == m ? 1.f : exp2_fast((m - next) * a.scale_log2);
             m = next;
@@ -194,57 +296,64 @@ template <typename E, int D, int NW> __global__ __launch_bounds__(64 * NW, 1) vo
                     o[db][r] *= down;
         }
         const float mc = finite_max(m) * a.scale_log2;
-        uint4 pf[4];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             float p[16];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 p[r] = exp2_fast(__builtin_fmaf(st[kb][r], a.scale_log2, -mc));
-                if (partly && (hidden >> (16 * kb + r) & 1))
-                    p[r] = 0.f;  // also where m is infinite
                 lsum += p[r];
-                st[kb][r] = p[r];
             }
             pf[2 * kb] = make_uint4(E::pack(p[0], p[1]), E::pack(p[2], p[3]), E::pack(p[4], p[5]), E::pack(p[6], p[7]));
             pf[2 * kb + 1] = make_uint4(E::pack(p[8], p[9]), E::pack(p[10], p[11]), E::pack(p[12], p[13]), E::pack(p[14], p[15]));
         }
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            const int r_lo = 16 * kk + 4 * half + (l % 16) / 4;
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-                const int c = db * 4 + 2 * (l / 16 % 2) + (l % 4) / 2;
-                const uint4 vf = lds_frag_tr(vt + Tile::v_at(r_lo, c) + 8 * (l % 2), vt + Tile::v_at(r_lo + 8, c) + 8 * (l % 2));
-                o[db] = E::mfma32(vf, pf[kk], o[db]);
-            }
+    };
+
+    // first keys of tiles t to t + 3
+    int j0 = first_key(0), j1 = first_key(1), j2 = first_key(2), j3 = first_key(3);
+    look_up(j0);
+    request(kChunkBuffers - 1, j0, 0, 0);
+    look_up(j1);
+    request(0, j1, 1, 1);
+    look_up(j2);
+    arrive(0, j0, 0);
+    lds_barrier();
+    if (late)
+        lds_barrier();
+    if (wave_works)
+        scores(0);
+    auto tile = [&](int t, int buf) __attribute__((always_inline)) {  // softmax of tile t, products behind it; false behind the last tile
+        const int next = (buf + 1) % kChunkBuffers, after = (buf + 2) % kChunkBuffers;
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        if (t + 1 < n)
+            request(next, j2, t + 2, after);
+        look_up(j3);
+        if (wave_works)
+            softmax(t, j0);
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        if (t + 1 >= n)
+            return false;
+        if (wave_works) {
+            products(buf, next);
+            not_finite_values(t, j0);
         }
-        if (bad != 0) {
-            for (uint64_t left = bad; left != 0; left &= left - 1) {
-                const int key = __builtin_ctzll(left), r = 4 * (key % 32 / 8) + key % 4, from = key % 8 / 4;
-                float p = 0.f;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        p = 16 * kb + e == 16 * (key / 32) + r ? st[kb][e] : p;
-                p = read_from(p, l % 32 + 32 * from);
-                const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
-                const bool sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key);
-                const uint16_t *v_row = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float v[4];
-                        unpack4<E>(*reinterpret_cast<const uint2 *>(v_row + db * 32 + 8 * q + 4 * half), v);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[db][4 * q + e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
-                    }
-            }
+        arrive(t + 1, j1, next);
+        j0 = j1, j1 = j2, j2 = j3, j3 = first_key(t + 4);
+        return true;
+    };
+    if (n > 0) {
+        for (int t = 0; tile(t, 0) && tile(t + 1, 1) && tile(t + 2, 2); t += kChunkBuffers) {
+        }
+        if (wave_works) {
+            values((n - 1) % kChunkBuffers);
+            not_finite_values(n - 1, j0);
         }
     }
+    memory_wait();
+    if (!late)
+        lds_barrier();
     if (!wave_works)
         return;
     lsum += read_from(lsum, l ^ 32);
@@ -294,7 +403,7 @@ template <int D> struct FewTile {
     static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4); }
 };
 
-template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves, 2) void attn_few_kernel(AttendArgs a)
+template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
 {
     typedef FewTile<D> Tile;
     constexpr int NT = 64 * kFewWaves, ROWS = 16 * RB, PIECES = Tile::kPieces;
@@ -348,8 +457,8 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
     uint4 kreg[2][KS], vreg[V_LOADS];
     int block = -1, row_of_key = -1;  // of key l % 32 of a tile: of the one behind the next, of the next
     uint64_t exist_next = 0;
-    auto look_up = [&](int step) { block = step < step_end ? table_entry(a, it.seq, keys.tile(step) * kFewKeys + l % 32, end) : -1; };
-    auto request = [&](int step) {
+    auto look_up = [&](int step) __attribute__((always_inline)) { block = step < step_end ? table_entry(a, it.seq, keys.tile(step) * kFewKeys + l % 32, end) : -1; };
+    auto request = [&](int step) __attribute__((always_inline)) {
         row_of_key = cache_row(a, block, kv_head, keys.tile(step) * kFewKeys + l % 32);
         exist_next = __ballot(row_of_key >= 0);
         const uint16_t *const k = static_cast<const uint16_t *>(a.k_cache), *const v = static_cast<const uint16_t *>(a.v_cache);
@@ -376,9 +485,10 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
         request(step_begin + wave);
         look_up(step_begin + wave + kFewWaves);
     }
+    const SeenTiles seen_tiles(a, keys.pos0, keys.pos1, kFewKeys);
     for (int step = step_begin + wave; step < step_end; step += kFewWaves) {
         const int j0 = keys.tile(step) * kFewKeys;
-        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kFewKeys);
+        const bool part_seen = !seen_tiles.all(j0);
         const uint32_t exist = (uint32_t)exist_next;
         f32x4 st[RB][2];
 #pragma unroll
@@ -416,20 +526,17 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
         uint4 pf[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            uint32_t hidden = 0;
             if (partly) {
+                const uint32_t keys_seen = (uint32_t)seen_keys(a, pos[rb], j0, exist), mine = keys_seen >> (4 * quarter);
+                seen[rb] = seen[rb] || keys_seen != 0;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int key = kb * 16 + 4 * quarter + r;
-                        const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos[rb], j0 + key);
-                        hidden |= sees_it ? 0u : 1u << (4 * kb + r);
-                        if (!sees_it)
-                            st[rb][kb][r] = -INFINITY;
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        st[rb][kb][r] = seen_score(st[rb][kb][r], mine, 16 * kb + r);
+            } else {
+                seen[rb] = true;
             }
-            seen[rb] = seen[rb] || hidden != 0xffu;
             float top = -INFINITY;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -453,8 +560,6 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 p[e] = exp2_fast(__builtin_fmaf(st[rb][e / 4][e % 4], a.scale_log2, -mc));
-                if (partly && (hidden >> e & 1))
-                    p[e] = 0.f;
                 lsum[rb] += p[e];
                 st[rb][e / 4][e % 4] = p[e];
             }
@@ -481,14 +586,14 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
                 for (int e = 0; e < 8; ++e)
                     p = e == e_of ? st[rb][e / 4][e % 4] : p;
                 p = read_from(p, l % 16 + 16 * from);
-                const bool sees_it = row_works[rb] && cr >= 0 && sees(a, pos[rb], j0 + key);
+                const uint32_t sees_it = row_works[rb] && cr >= 0 && sees(a, pos[rb], j0 + key) ? ~0u : 0u;
 #pragma unroll
                 for (int db = 0; db < D / 16; ++db) {
                     float v[4];
                     unpack4<E>(*reinterpret_cast<const uint2 *>(v_row + db * 16 + 4 * quarter), v);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        o[rb][db][e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
+                        o[rb][db][e] += not_finite_part(p, v[e], sees_it);
                 }
             }
         }
@@ -608,13 +713,13 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     float4 kreg[LOADS], vreg[LOADS];
     int block[LOADS];
     int there = 0;
-    auto look_up = [&](int step) {
+    auto look_up = [&](int step) __attribute__((always_inline)) {
         const int j0 = keys.tile(step) * kF32Keys;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
             block[i] = step < step_end ? table_entry(a, it.seq, j0 + load_row + i * ROWS_PER_LOAD, end) : -1;
     };
-    auto request = [&](int step) {
+    auto request = [&](int step) __attribute__((always_inline)) {
         const int j0 = keys.tile(step) * kF32Keys;
         there = 0;
 #pragma unroll
@@ -634,9 +739,10 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         request(step_begin);
         look_up(step_begin + 1);
     }
+    const SeenTiles seen_tiles(a, keys.pos0, keys.pos1, kF32Keys);
     for (int step = step_begin; step < step_end; ++step) {
         const int j0 = keys.tile(step) * kF32Keys;
-        const bool part_seen = !all_see(a, keys.pos0, keys.pos1, j0, kF32Keys);
+        const bool part_seen = !seen_tiles.all(j0);
         lds_barrier();  // the tile in front has been read
         if (tid < kF32Keys)
             lds_bad[tid] = 0;
@@ -677,20 +783,17 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         }
         const uint32_t exist = (uint32_t)__ballot(flag[l % 32] != 0), bad = (uint32_t)__ballot(lds_bad[l % 32] != 0);
         const bool partly = part_seen || exist != 0xffffffffu;
-        uint32_t hidden = 0;
         if (partly) {
+            const uint32_t keys_seen = (uint32_t)seen_keys(a, pos, j0, exist), mine = keys_seen >> (4 * quarter);
+            seen = seen || keys_seen != 0;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int key = kb * 16 + 4 * quarter + r;
-                    const bool sees_it = (exist >> key & 1) != 0 && sees(a, pos, j0 + key);
-                    hidden |= sees_it ? 0u : 1u << (4 * kb + r);
-                    if (!sees_it)
-                        st[kb][r] = -INFINITY;
-                }
+                for (int r = 0; r < 4; ++r)
+                    st[kb][r] = seen_score(st[kb][r], mine, 16 * kb + r);
+        } else {
+            seen = true;
         }
-        seen = seen || hidden != 0xffu;
         float top = -INFINITY;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
@@ -712,9 +815,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         const float mc = finite_max(m) * a.scale_log2;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            float p = exp2_fast(__builtin_fmaf(st[e / 4][e % 4], a.scale_log2, -mc));
-            if (partly && (hidden >> e & 1))
-                p = 0.f;
+            const float p = exp2_fast(__builtin_fmaf(st[e / 4][e % 4], a.scale_log2, -mc));
             lsum += p;
             st[e / 4][e % 4] = p;
         }
@@ -734,14 +835,14 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
             for (int e = 0; e < 8; ++e)
                 p = e == e_of ? st[e / 4][e % 4] : p;
             p = read_from(p, l % 16 + 16 * from);
-            const bool sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key);
+            const uint32_t sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key) ? ~0u : 0u;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
                 const float4 x = *reinterpret_cast<const float4 *>(v_row + db * 16 + 4 * quarter);
                 const float v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    o[db][e] += sees_it && not_finite(v[e]) ? p * v[e] : 0.f;
+                    o[db][e] += not_finite_part(p, v[e], sees_it);
             }
         }
     }
@@ -944,10 +1045,15 @@ template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Laun
 {
     hipError_t e;
     if (chunk) {
-        constexpr size_t lds = 4 * (size_t)ChunkTile<D>::kBytes + (2 * kChunkKeys + 2 * kChunkWaves + 8) * sizeof(int);
-        if ((e = lds_limit(attn_chunk_kernel<E, D, kChunkWaves>, lds)) != hipSuccess)
+        constexpr size_t lds = 2 * kChunkBuffers * (size_t)ChunkTile<D>::kBytes + (8 * kChunkKeys + 2 * kChunkWaves + 8) * sizeof(int);
+        const bool wide = 1 << a.log2_bs >= kChunkKeys / kChunkWaves;
+        e = wide ? lds_limit(attn_chunk_kernel<E, D, kChunkWaves, true>, lds) : lds_limit(attn_chunk_kernel<E, D, kChunkWaves, false>, lds);
+        if (e != hipSuccess)
             return e;
-        hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
+        if (wide)
+            hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves, true>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
+        else
+            hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves, false>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
         e = hipGetLastError();
     } else {
         e = c.rows == 16 ? launch_few<E, D, 1>(a, c, stream) : c.rows == 32 ? launch_few<E, D, 2>(a, c, stream) : launch_few<E, D, 4>(a, c, stream);
@@ -1005,7 +1111,7 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.log2_bs = __builtin_ctz((unsigned)s.block_size);
     a.max_blocks = max_blocks;
     a.n_blocks = n_blocks;
-    a.window = window;
+    a.window = window < kMostWindow ? window : kMostWindow;
     a.sinks = sinks;
     a.scale_log2 = scale * kLog2e;
     unsigned char *ws = static_cast<unsigned char *>(workspace);

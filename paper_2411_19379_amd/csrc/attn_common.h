@@ -10,6 +10,7 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kMaxBatch = 4096;
+constexpr int kMostWindow = 0x7fffff00;  // differences of positions and windows stay within 32 bits
 
 // ---------------------------------------------------------------- lanes and waves
 __device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
@@ -22,6 +23,40 @@ __device__ __forceinline__ float read_from(float v, int lane)
 // LDS is ordered, loads in flight stay in flight
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Where a pointer into LDS points, as the copies below want it.
+__device__ __forceinline__ uint32_t lds_address(const void *p)
+{
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
+}
+// 16 bytes per lane from memory right into LDS: lane l's, `offset` bytes behind `from`, go to `to` + 16 l; `from` and `to` are
+// the same for the whole wave.  They are there after the wave's next memory_wait(); the wave must wait before it ends.  (M0
+// holds nothing else in these kernels: there is no other use of it in what is compiled.)
+__device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t offset, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to) : "memory");
+}
+// The same with an address per lane.
+__device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+}
+__device__ __forceinline__ void memory_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A pointer in scalar registers of its own.  Arguments are loaded sixteen registers at a time, and kept, spilled and read back
+// like that for the sake of one of them.
+__device__ __forceinline__ const unsigned char *own_pointer(const void *p)
+{
+    asm volatile("" : "+s"(p));
+    return static_cast<const unsigned char *>(p);
+}
+// The value, of which the compiler knows nothing: what rare branches compute from it stays in them instead of taking registers
+// of the loops around them.
+__device__ __forceinline__ int unknown(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return a + b < a ? 0xffffffffu : a + b; }
 
@@ -113,11 +148,32 @@ __device__ __forceinline__ bool sees(const AttendArgs &a, int pos, int j)
 {
     return j <= pos && (a.window <= 0 || pos - j < a.window || j < a.sinks);
 }
-// Every row at positions pos0..pos1 sees every key of [j0, j0 + n).
-__device__ __forceinline__ bool all_see(const AttendArgs &a, int pos0, int pos1, int j0, int n)
+// Which of the N <= 64 keys from j0 on the query at `pos` sees, of those that exist: bit k is key j0 + k.
+__device__ __forceinline__ uint64_t first_bits(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint64_t seen_keys(const AttendArgs &a, int pos, int j0, uint64_t exist)
 {
-    return j0 + n - 1 <= pos0 && (a.window <= 0 || pos1 - j0 < a.window || j0 + n <= a.sinks);
+    uint64_t m = exist & first_bits(pos - j0 + 1);
+    if (a.window > 0)
+        m &= ~first_bits(pos - j0 - a.window + 1) | first_bits(a.sinks - j0);
+    return m;
 }
+// The score, or minus infinity (a weight of 0 in any case) if `bit` of the keys that are seen is not set: two bit operations and
+// no condition register.
+__device__ __forceinline__ float seen_score(float score, uint32_t keys, int bit)
+{
+    const uint32_t is = (uint32_t)((int)(keys << (31 - bit)) >> 31);
+    return __uint_as_float((__float_as_uint(score) & is) | (0xff800000u & ~is));
+}
+
+// Of which tiles of n keys every row at positions pos0..pos1 sees every key.
+struct SeenTiles {
+    int last, behind, sinks;  // first keys: up to `last` and behind `behind`, or up to `sinks`
+    __device__ __forceinline__ SeenTiles(const AttendArgs &a, int pos0, int pos1, int n)
+        : last(pos0 - n + 1), behind(a.window > 0 ? pos1 - a.window : -1), sinks(a.sinks - n)
+    {
+    }
+    __device__ __forceinline__ bool all(int j0) const { return j0 <= last && (j0 > behind || j0 <= sinks); }
+};
 
 // ---------------------------------------------------------------- who does what
 // The rows of a sequence are cut into tiles of ROWS rows; the keys of all tiles of a sequence into the same number of
@@ -265,6 +321,13 @@ template <typename E> __device__ __forceinline__ bool drop_not_finite(uint32_t &
 }
 
 __device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+
+// p v where v is not finite and the row sees its key (sees: all bits, or none), else 0, without a condition register.
+__device__ __forceinline__ float not_finite_part(float p, float v, uint32_t sees)
+{
+    const uint32_t is = (uint32_t)((int)((__float_as_uint(v) & 0x7f800000u) + 0x00800000u) >> 31);
+    return __uint_as_float(__float_as_uint(p * v) & is & sees);
+}
 
 // Weight of a row's maximum: 0 where nothing finite has been seen yet, so that no infinity is subtracted from itself.
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }

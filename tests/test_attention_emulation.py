@@ -17,6 +17,22 @@ from test_kernel_emulation import CLANG, CSRC, EMU, ROOT, _convert
 HERE = os.path.join(ROOT, "tests", "attn_emu")
 
 
+# Copies from memory into LDS, and the wait for them, which either run at once or (EMU_LATE_COPIES) only when they are waited for:
+# the one shows a copy that overwrites what is still read, the other a read in front of the wait.
+_LOAD = 'global_load_lds_dwordx4 %0, '
+_COPIES = [
+    ("    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;",
+     "    return (uint32_t)(static_cast<const unsigned char *>(p) - emu::lds_base());"),
+    ('    asm volatile("s_mov_b32 m0, %2\\n\\ts_nop 0\\n\\t' + _LOAD + '%1" ::"v"(offset), "s"(from), "s"(to) : "memory");\n',
+     "    emu::copy16_to_lds(static_cast<const unsigned char *>(from) + offset, to, __LINE__);\n"),
+    ('    asm volatile("s_mov_b32 m0, %1\\n\\ts_nop 0\\n\\t' + _LOAD + 'off" ::"v"(from), "s"(to) : "memory");\n',
+     "    emu::copy16_to_lds(from, to, __LINE__);\n"),
+    ('    asm volatile("" : "+s"(p));\n', ""),
+    ('    asm volatile("" : "+v"(v));\n', ""),
+    ("""asm volatile("s_waitcnt vmcnt(0)" ::: "memory");""", "emu::memory_wait(__LINE__);"),
+]
+
+
 @pytest.fixture(scope="session")
 def emu(tmp_path_factory):
     if not os.path.exists(CLANG):
@@ -26,7 +42,12 @@ def emu(tmp_path_factory):
     for name in ("attn_step", "attn_attend"):
         _convert(os.path.join(CSRC, name + ".hip"), os.path.join(d, name + ".cpp"))
         srcs.append(os.path.join(d, name + ".cpp"))
-    _convert(os.path.join(CSRC, "attn_common.h"), os.path.join(d, "attn_common.h"))
+    common = open(os.path.join(CSRC, "attn_common.h")).read()
+    for asm, call in _COPIES:
+        assert common.count(asm) == 1, asm
+        common = common.replace(asm, call)
+    open(os.path.join(d, "common.h"), "w").write(common)
+    _convert(os.path.join(d, "common.h"), os.path.join(d, "attn_common.h"))
     flags = ["-std=c++17", "-O2", "-fno-strict-aliasing", "-ffp-contract=off", "-Wno-psabi", "-Wno-unused-value",
              "-DATTN_TARGET=emu::env_int(\"EMU_TARGET\")", "-I", d, "-I", HERE, "-I", EMU, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     procs = [subprocess.Popen([CLANG, *flags, "-c", s, "-o", os.path.join(d, f"{i}.o")], stderr=subprocess.PIPE, text=True)
@@ -45,7 +66,7 @@ def _bits(t):
     return (t.view(torch.int32) if t.dtype == torch.float32 else t.view(torch.int16)).numpy().tobytes()
 
 
-def _run(exe, tmp_path, op, params, arrays, order=0, side="end", target=0):
+def _run(exe, tmp_path, op, params, arrays, order=0, side="end", target=0, late=0):
     src, dst = str(tmp_path / "in.bin"), str(tmp_path / "out.bin")
     words = np.zeros(34, np.int32)
     words[0], words[1] = 0x4154544e, op
@@ -54,13 +75,13 @@ def _run(exe, tmp_path, op, params, arrays, order=0, side="end", target=0):
         f.write(words.tobytes())
         for a in arrays:
             f.write(a if isinstance(a, bytes) else np.ascontiguousarray(a).tobytes())
-    env = dict(os.environ, EMU_TARGET=str(target))
+    env = dict(os.environ, EMU_TARGET=str(target), EMU_LATE_COPIES=str(late))
     r = subprocess.run([exe, src, dst, str(order), side], capture_output=True, text=True, timeout=600, env=env)
     assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
     return open(dst, "rb").read()
 
 
-def _attend(exe, tmp_path, p, order=0, side="end", target=0, gap=0):
+def _attend(exe, tmp_path, p, order=0, side="end", target=0, gap=0, late=0):
     """`gap`: elements between the tokens of q beyond their heads."""
     row = p.hq * p.d
     q = torch.full((p.T, row + gap), float("nan"), dtype=p.q.dtype)
@@ -69,7 +90,7 @@ def _attend(exe, tmp_path, p, order=0, side="end", target=0, gap=0):
     params = [p.hq, p.hkv, p.d, p.bs, ah.CODE[p.dtype], p.T, len(p.new), p.k_cache.shape[0], p.table.shape[1], p.window, p.sinks,
               p.max_new, int(np.float32(p.scale).view(np.int32)), row + gap]
     raw = _run(exe, tmp_path, 2, params, [_bits(flat), _bits(p.k_cache), _bits(p.v_cache), p.table, p.cu, np.array(p.cached, np.int32)],
-               order, side, target)
+               order, side, target, late)
     esz = p.q.element_size()
     n = p.T * row
     out = torch.frombuffer(bytearray(raw[:n * esz]) or bytearray(esz), dtype=p.q.dtype)[:n].double().numpy().reshape(p.T, p.hq, p.d)
@@ -103,8 +124,8 @@ def test_attend(emu, tmp_path, name, target):
     p = ah.make(11, *CASES[name])
     out, lse = _attend(emu, tmp_path, p, target=target)
     ah.check(p, out, lse, name)
-    for order, side in ((1, "start"), (5, "end")):
-        other = _attend(emu, tmp_path, p, order, side, target)
+    for order, side, late in ((1, "start", 1), (5, "end", 0), (4, "end", 1)):
+        other = _attend(emu, tmp_path, p, order, side, target, late=late)
         assert np.array_equal(out, other[0]) and np.array_equal(lse, other[1]), f"{name}: order {order} changes the result"
 
 
