@@ -248,9 +248,9 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
                 two = w == word ? (w % 4 == 0 ? f.x : w % 4 == 1 ? f.y : w % 4 == 2 ? f.z : f.w) : two;
             }
             const float p = read_from(key % 2 ? E::hi(two) : E::lo(two), l % 32 + 32 * from);
-            const int j = j0 + key, cr = cache_row(a, table_entry(a, it.seq, j, end), kv_head, j);
+            const int j = j0 + key, e = j >> a.log2_bs, cr = cache_row(a, j < end && e < a.max_blocks ? table[e] : -1, kv_head, j);
             const uint32_t sees_it = row_works && cr >= 0 && sees(a, pos, j) ? ~0u : 0u;
-            const uint16_t *v_of = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
+            const uint16_t *v_of = reinterpret_cast<const uint16_t *>(v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
 #pragma unroll

@@ -43,19 +43,21 @@ __device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t to)
 }
 __device__ __forceinline__ void memory_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// A pointer in scalar registers of its own.  Arguments are loaded sixteen registers at a time, and kept, spilled and read back
-// like that for the sake of one of them.
-__device__ __forceinline__ const unsigned char *own_pointer(const void *p)
-{
-    asm volatile("" : "+s"(p));
-    return static_cast<const unsigned char *>(p);
-}
 // The value, of which the compiler knows nothing: what rare branches compute from it stays in them instead of taking registers
 // of the loops around them.
 __device__ __forceinline__ int unknown(int v)
 {
     asm volatile("" : "+v"(v));
     return v;
+}
+
+// A pointer, the same in all lanes, in scalar registers of its own.  Arguments are loaded sixteen registers at a time, and kept,
+// spilled and read back like that for the sake of one of them.
+__device__ __forceinline__ const unsigned char *own_pointer(const void *p)
+{
+    const uint64_t u = (uint64_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane(unknown((int)(uint32_t)u)), hi = (uint32_t)__builtin_amdgcn_readfirstlane(unknown((int)(u >> 32)));
+    return (const unsigned char *)((uint64_t)hi << 32 | lo);
 }
 
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return a + b < a ? 0xffffffffu : a + b; }

@@ -27,7 +27,6 @@ _COPIES = [
      "    emu::copy16_to_lds(static_cast<const unsigned char *>(from) + offset, to, __LINE__);\n"),
     ('    asm volatile("s_mov_b32 m0, %1\\n\\ts_nop 0\\n\\t' + _LOAD + 'off" ::"v"(from), "s"(to) : "memory");\n',
      "    emu::copy16_to_lds(from, to, __LINE__);\n"),
-    ('    asm volatile("" : "+s"(p));\n', ""),
     ('    asm volatile("" : "+v"(v));\n', ""),
     ("""asm volatile("s_waitcnt vmcnt(0)" ::: "memory");""", "emu::memory_wait(__LINE__);"),
 ]
