@@ -10,9 +10,12 @@ workspace are torch tensors.  There is no CPU fallback: loading raises if the li
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import NamedTuple, Optional
+
+import torch  # owns device memory and streams; its HIP runtime is the one the library has to bind to
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libattn_cache.so")
@@ -45,9 +48,6 @@ def load_library():
     global _lib
     if _lib is not None:
         return _lib
-    # PyTorch owns device memory and streams here: its HIP runtime is the one this library has to bind to
-    import torch  # noqa: F401
-
     if not os.path.exists(_LIB_PATH):
         raise FileNotFoundError(f"{_LIB_PATH} is not built: run `python -m paper_2411_19379_amd.build`")
     lib = ctypes.CDLL(_LIB_PATH)
@@ -84,42 +84,71 @@ def attn_workspace_bytes(shape: AttnShape, batch: int, total_tokens: int, max_ne
     return n.value
 
 
-def _dtype_code(dtype) -> int:
-    import torch
+# A decode step of one layer is a few microseconds of GPU work and each line here costs a tenth of one: what follows from sizes
+# alone is kept, and tensors are checked in one expression each.
+_DTYPES = {torch.float32: ATTN_DT_F32, torch.bfloat16: ATTN_DT_BF16, torch.float16: ATTN_DT_F16}
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+# the raw handle of a GPU's current stream, without the object that torch.cuda.current_stream makes where there is a way
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    code = {torch.float32: ATTN_DT_F32, torch.bfloat16: ATTN_DT_BF16, torch.float16: ATTN_DT_F16}.get(dtype)
-    if code is None:
+
+@functools.lru_cache(maxsize=256)
+def _shape_of(n_q_heads, n_kv_heads, head_dim, block_size, dtype):
+    """The address of the shape."""
+    if dtype not in _DTYPES:
         raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    return code
+    return ctypes.byref(AttnShape(n_q_heads, n_kv_heads, head_dim, block_size, _DTYPES[dtype]))
 
 
-def _tensor(name, t, shape, dtype, device):
-    """A contiguous tensor of this shape (None: any extent) and type on `device`."""
-    if t.dtype != dtype or t.dim() != len(shape) or t.device != device or not t.is_contiguous() \
-            or any(want is not None and have != want for have, want in zip(t.shape, shape)):
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+@functools.lru_cache(maxsize=4096)
+def _workspace_of(n_q_heads, n_kv_heads, head_dim, block_size, dtype, batch, total_tokens, max_new):
+    shape = AttnShape(n_q_heads, n_kv_heads, head_dim, block_size, _DTYPES[dtype])
+    return attn_workspace_bytes(shape, batch, total_tokens, max_new)
+
+
+def _refuse(name, t, shape, dtype, index):
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
+
+
+def _ints(name, t, n, index):
+    """The address of n contiguous int32 values on GPU `index` (n None: any number)."""
+    if t.dtype is not _I32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        _refuse(name, t, (n,), _I32, index)
     return t.data_ptr()
 
 
-def _heads(name, t, shape, dtype, device):
+def _rows(name, t, n, index):
+    """The address and the width of n contiguous rows of int32 values."""
+    have = t.shape
+    if t.dtype is not _I32 or t.get_device() != index or len(have) != 2 or have[0] != n or not t.is_contiguous():
+        _refuse(name, t, (n, "any"), _I32, index)
+    return t.data_ptr(), have[1]
+
+
+def _tensor(name, t, shape, dtype, index):
+    """The address of a contiguous tensor."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, index)
+    return t.data_ptr()
+
+
+def _heads(name, t, shape, dtype, index):
     """[tokens, heads, head_dim] whose heads are contiguous; returns the address and the elements between tokens."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
-        raise ValueError(f"{name}: expected a {dtype} tensor of shape {shape} on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(name, t, shape, dtype, index)
     tokens, heads, dim = t.stride()
-    row = shape[1] * shape[2]
     if (dim != 1 and shape[2] > 1) or (heads != shape[2] and shape[1] > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous, got strides {t.stride()}")
-    return t.data_ptr(), (tokens if shape[0] > 1 else row)
+    return t.data_ptr(), (tokens if shape[0] > 1 else shape[1] * shape[2])
 
 
 def _device(t):
-    import torch
-
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    """The index of the current GPU, which the tensor has to be on."""
+    index = t.get_device()
+    if index < 0 or index != torch.cuda.current_device():
         raise ValueError(f"expected tensors on the current CUDA device, got {t.device}")
-    return t.device
+    return index
 
 
 class Step(NamedTuple):
@@ -135,25 +164,18 @@ def assign_blocks(block_size: int, total_tokens: int, cu_seqlens, cached_lens, t
                   shared_tail=None, in_place: bool = False) -> Step:
     """Blocks, slots and positions of the new tokens of a batch.  `n_free` is a device int32 tensor of one value; the
     next step's is `counts[:1]` of this one.  `in_place` extends the rows of `table`, else they are written to a new one."""
-    import torch
-
     dev = _device(cu_seqlens)
-    i32 = torch.int32
     batch = cu_seqlens.numel() - 1
-    cu = _tensor("cu_seqlens", cu_seqlens, (batch + 1,), i32, dev)
-    cached = _tensor("cached_lens", cached_lens, (batch,), i32, dev)
-    tab = _tensor("table", table, (batch, None), i32, dev)
-    free = _tensor("free_blocks", free_blocks, (None,), i32, dev)
-    n = _tensor("n_free", n_free, (1,), i32, dev)
-    shared = _tensor("shared_tail", shared_tail, (batch,), i32, dev) if shared_tail is not None else None
+    tab, width = _rows("table", table, batch, dev)
     out = table if in_place else torch.empty_like(table)
-    slots = torch.empty((total_tokens,), dtype=torch.int64, device=dev)
-    small = torch.empty((total_tokens + 4 * batch + 2,), dtype=i32, device=dev)
-    positions, copies, counts = small[:total_tokens], small[total_tokens:-2].view(batch, 4), small[-2:]
+    slots = torch.empty((total_tokens,), dtype=_I64, device=table.device)
+    positions, copies, counts = table.new_empty((total_tokens,)), table.new_empty((batch, 4)), table.new_empty((2,))
     _check(load_library().attn_assign_blocks(
-        batch, block_size, table.shape[1], total_tokens, cu, cached, shared, tab, out.data_ptr(), free, n,
-        free_blocks.numel(), slots.data_ptr(), positions.data_ptr(), copies.data_ptr(), counts.data_ptr(),
-        torch.cuda.current_stream(dev).cuda_stream))
+        batch, block_size, width, total_tokens, _ints("cu_seqlens", cu_seqlens, batch + 1, dev),
+        _ints("cached_lens", cached_lens, batch, dev),
+        None if shared_tail is None else _ints("shared_tail", shared_tail, batch, dev), tab, out.data_ptr(),
+        _ints("free_blocks", free_blocks, None, dev), _ints("n_free", n_free, 1, dev), free_blocks.numel(), slots.data_ptr(),
+        positions.data_ptr(), copies.data_ptr(), counts.data_ptr(), _stream(dev)))
     return Step(out, slots, positions, copies, counts)
 
 
@@ -165,8 +187,6 @@ def rotary_table(max_positions: int, rotary_dim: int, base: float = 10000.0, *, 
     interpolation by parts of arXiv 2309.00071) divides by that factor the frequencies that turn fewer than `slow_turns` times over
     the trained positions, keeps those that turn more than `fast_turns` times, goes over linearly between, and scales cos and
     sin by 0.1 ln(by_parts) + 1."""
-    import torch
-
     if max_positions < 1 or rotary_dim < 16 or rotary_dim % 16:
         raise ValueError("max_positions must be positive, rotary_dim a positive multiple of 16")
     if linear < 1.0 or by_parts < 1.0 or not slow_turns < fast_turns:
@@ -179,43 +199,42 @@ def rotary_table(max_positions: int, rotary_dim: int, base: float = 10000.0, *, 
     return torch.stack([angle.cos() * size, angle.sin() * size], 1).float().contiguous().to(device)
 
 
-def _cache_shape(k_cache, v_cache, n_q_heads, dtype, device):
-    if k_cache.dim() != 4:
-        raise ValueError(f"k_cache: expected [n_blocks, n_kv_heads, block_size, head_dim], got {tuple(k_cache.shape)}")
-    n_blocks, n_kv, bs, d = k_cache.shape
-    _tensor("k_cache", k_cache, (n_blocks, n_kv, bs, d), dtype, device)
-    _tensor("v_cache", v_cache, (n_blocks, n_kv, bs, d), dtype, device)
-    return n_blocks, AttnShape(n_q_heads, n_kv, d, bs, _dtype_code(dtype))
+def _caches(k_cache, v_cache, dtype, index):
+    """The caches' extents and addresses."""
+    extents = k_cache.shape
+    if len(extents) != 4:
+        raise ValueError(f"k_cache: expected [n_blocks, n_kv_heads, block_size, head_dim], got {tuple(extents)}")
+    return extents, _tensor("k_cache", k_cache, extents, dtype, index), _tensor("v_cache", v_cache, extents, dtype, index)
 
 
 def rope_append(q, k, v, positions, slots, rotary, k_cache, v_cache, *, interleaved: bool = False, copies=None, q_out=None):
     """Rotary positions on q and k, k and v into the cache; returns the turned q [tokens, n_q_heads, head_dim].
     q, k and v may be parts of one projection's rows.  `rotary` is a `rotary_table` or None, `copies` comes from
     `assign_blocks` where sequences share their tails."""
-    import torch
-
     dev, dtype = _device(q), q.dtype
-    T, hq = q.shape[0], q.shape[1]
-    n_blocks, shape = _cache_shape(k_cache, v_cache, hq, dtype, dev)
-    d, hkv = shape.head_dim, shape.n_kv_heads
-    qp, qs = _heads("q", q, (T, hq, d), dtype, dev)
-    kp, ks = _heads("k", k, (T, hkv, d), dtype, dev)
-    vp, vs = _heads("v", v, (T, hkv, d), dtype, dev)
-    slot = _tensor("slots", slots, (T,), torch.int64, dev)
+    T, hq = q.shape[:2]
+    (n_blocks, hkv, bs, d), k_to, v_to = _caches(k_cache, v_cache, dtype, dev)
+    shape = _shape_of(hq, hkv, d, bs, dtype)
+    q_shape, kv_shape = (T, hq, d), (T, hkv, d)
+    qp, qs = _heads("q", q, q_shape, dtype, dev)
+    kp, ks = _heads("k", k, kv_shape, dtype, dev)
+    vp, vs = _heads("v", v, kv_shape, dtype, dev)
     pos = table = copy = None
     most = rot = batch = 0
     if rotary is not None:
-        pos = _tensor("positions", positions, (T,), torch.int32, dev)
-        table = _tensor("rotary", rotary, (None, 2, None), torch.float32, dev)
-        most, rot = rotary.shape[0], 2 * rotary.shape[2]
+        pos = _ints("positions", positions, T, dev)
+        if rotary.dim() != 3 or rotary.shape[1] != 2:
+            raise ValueError(f"rotary: expected [positions, 2, rotary_dim / 2], got {tuple(rotary.shape)}")
+        most, _, rot = rotary.shape
+        table, rot = _tensor("rotary", rotary, (most, 2, rot), _F32, dev), 2 * rot
     if copies is not None:
-        copy, batch = _tensor("copies", copies, (None, 4), torch.int32, dev), copies.shape[0]
+        batch = copies.shape[0]
+        copy = _tensor("copies", copies, (batch, 4), _I32, dev)
     if q_out is None:
-        q_out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-    out = _tensor("q_out", q_out, (T, hq, d), dtype, dev)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
     _check(load_library().attn_rope_append(
-        ctypes.byref(shape), T, batch, n_blocks, qp, qs, kp, ks, vp, vs, pos, slot, table, most, rot, int(interleaved),
-        copy, out, k_cache.data_ptr(), v_cache.data_ptr(), torch.cuda.current_stream(dev).cuda_stream))
+        shape, T, batch, n_blocks, qp, qs, kp, ks, vp, vs, pos, _tensor("slots", slots, (T,), _I64, dev), table, most, rot,
+        int(interleaved), copy, _tensor("q_out", q_out, q_shape, dtype, dev), k_to, v_to, _stream(dev)))
     return q_out
 
 
@@ -224,26 +243,22 @@ def attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, *, scale: Option
     """Attention of the new tokens over the cache.  Returns out [tokens, n_q_heads, head_dim], with `return_lse` also the
     log of the sum of exponentials [tokens, n_q_heads].  `scale` is 1 / sqrt(head_dim) if not given; `max_new`, the largest
     number of new tokens of any sequence, picks the faster kernel (0: not known)."""
-    import torch
-
     dev, dtype = _device(q), q.dtype
-    T, hq = q.shape[0], q.shape[1]
-    n_blocks, shape = _cache_shape(k_cache, v_cache, hq, dtype, dev)
-    d = shape.head_dim
+    T, hq = q.shape[:2]
+    (n_blocks, hkv, bs, d), kp, vp = _caches(k_cache, v_cache, dtype, dev)
+    shape = _shape_of(hq, hkv, d, bs, dtype)
     batch = cu_seqlens.numel() - 1
-    qp, qs = _heads("q", q, (T, hq, d), dtype, dev)
-    tab = _tensor("table", table, (batch, None), torch.int32, dev)
-    cu = _tensor("cu_seqlens", cu_seqlens, (batch + 1,), torch.int32, dev)
-    cached = _tensor("cached_lens", cached_lens, (batch,), torch.int32, dev)
+    q_shape = (T, hq, d)
+    qp, qs = _heads("q", q, q_shape, dtype, dev)
+    tab, width = _rows("table", table, batch, dev)
     if out is None:
-        out = torch.empty((T, hq, d), dtype=dtype, device=dev)
-    op, os_ = _heads("out", out, (T, hq, d), dtype, dev)
-    lse = torch.empty((T, hq), dtype=torch.float32, device=dev) if return_lse else None
-    need = attn_workspace_bytes(shape, batch, T, max_new)
-    ws = torch.empty((need,), dtype=torch.uint8, device=dev) if need else None
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    op, os_ = _heads("out", out, q_shape, dtype, dev)
+    lse = torch.empty((T, hq), dtype=_F32, device=q.device) if return_lse else None
+    need = _workspace_of(hq, hkv, d, bs, dtype, batch, T, max_new)
+    ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
     _check(load_library().attn_attend(
-        ctypes.byref(shape), batch, T, n_blocks, table.shape[1], qp, qs, k_cache.data_ptr(), v_cache.data_ptr(), tab, cu,
-        cached, 1.0 / math.sqrt(d) if scale is None else scale, window, sinks, max_new, op, os_,
-        lse.data_ptr() if return_lse else None, ws.data_ptr() if need else None, need,
-        torch.cuda.current_stream(dev).cuda_stream))
+        shape, batch, T, n_blocks, width, qp, qs, kp, vp, tab, _ints("cu_seqlens", cu_seqlens, batch + 1, dev),
+        _ints("cached_lens", cached_lens, batch, dev), 1.0 / math.sqrt(d) if scale is None else scale, window, sinks, max_new,
+        op, os_, lse.data_ptr() if return_lse else None, ws.data_ptr() if need else None, need, _stream(dev)))
     return (out, lse) if return_lse else out

@@ -876,9 +876,12 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 }
 
 // ================================================================ joining
-// The rows of sequences whose keys were split: 16 lanes per row, partial results in their order.
+// The rows of sequences whose keys were split, a wave per row: the lanes load the maxima and weights of up to 64 parts at once,
+// then the sums in the order of the parts, 64 * 4 / D parts per load and kJoinAhead loads on their way.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = kJoinThreads / 16;
+constexpr int kJoinRows = kJoinThreads / 64;
+constexpr int kJoinAhead = 4;
+constexpr int kJoinWorkgroups = 1024;
 
 template <typename E> struct Out {
     static __device__ __forceinline__ void store4(void *out, int64_t at, const float *v)
@@ -893,51 +896,88 @@ template <> struct Out<float> {
     }
 };
 
-template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a)
+// Row `in_tile` of a tile of rows; called by whole waves.
+template <typename E, int D, int ROWS> __device__ __forceinline__ void join_row(const AttendArgs &a, const Item &it, const Seq &s, int kv_head, int in_tile)
 {
-    constexpr int BLOCKS = ROWS / kJoinRows;  // workgroups per (tile, key head)
-    extern __shared__ __align__(16) unsigned char lds_raw[];
-    const int piece = blockIdx.x % BLOCKS, kv_head = blockIdx.x / BLOCKS % a.Hkv;
-    Item it;
-    if (!find_item<kJoinThreads, ROWS, KT>(a, blockIdx.x / BLOCKS / a.Hkv, true, reinterpret_cast<int *>(lds_raw), &it))
-        return;
-    const Seq s = load_seq(a, it.seq);
-    const int in_tile = piece * kJoinRows + threadIdx.x / 16, row = it.tile * ROWS + in_tile;
+    constexpr int LANES = D / 4, PARTS = 64 / LANES;  // lanes of a part's row, parts per load
+    const int l = lane_id(), row = it.tile * ROWS + in_tile;
     if (row >= s.rows || part_of(a, it, kv_head, it.n_splits - 1) >= a.most_parts)
         return;
     const float *const ml = a.part + (int64_t)a.most_parts * a.rows_cap * D;
-    JoinedRow j;
-    for (int p = 0; p < it.n_splits; ++p)
-        j.add_max(ml[((int64_t)part_of(a, it, kv_head, p) * a.rows_cap + in_tile) * 2]);
-    float v[D / 64][4];
+    const int token = row / a.group, head = kv_head * a.group + row - token * a.group;
+    auto at = [&](int p) __attribute__((always_inline)) { return (int64_t)part_of(a, it, kv_head, p) * a.rows_cap + in_tile; };
+
+    float m = -INFINITY;
+    for (int p0 = 0; p0 < it.n_splits; p0 += 64)
+        if (p0 + l < it.n_splits)
+            m = fmaxf(m, ml[at(p0 + l) * 2]);
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
+    for (int d = 1; d < 64; d *= 2)
+        m = fmaxf(m, read_from(m, l ^ d));
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, weight = 0.f;
+    int undefined = 0;
+    for (int p0 = 0; p0 < it.n_splits; p0 += 64) {
+        const int n = it.n_splits - p0 < 64 ? it.n_splits - p0 : 64;
+        JoinedRow j;
+        j.m = m;
+        float factor = 0.f;  // of part p0 + l
+        if (l < n) {
+            const float2 x = *reinterpret_cast<const float2 *>(ml + at(p0 + l) * 2);
+            factor = j.add_weight(x.x, x.y, a.scale_log2);
+        }
+        weight += j.w;
+        undefined |= (int)j.undefined;
+        for (int p1 = 0; p1 < n; p1 += PARTS * kJoinAhead) {
+            float4 x[kJoinAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[i][e] = 0.f;
-    for (int p = 0; p < it.n_splits; ++p) {
-        const int64_t at = (int64_t)part_of(a, it, kv_head, p) * a.rows_cap + in_tile;
-        const float2 x = *reinterpret_cast<const float2 *>(ml + at * 2);
-        const float w = j.add_weight(x.x, x.y, a.scale_log2);
-        if (w != 0.f) {
+            for (int u = 0; u < kJoinAhead; ++u) {
+                const int p = p1 + u * PARTS + l / LANES;
+                x[u] = *reinterpret_cast<const float4 *>(a.part + at(p0 + (p < n ? p : n - 1)) * D + 4 * (l % LANES));
+            }
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i) {
-                const float4 o = *reinterpret_cast<const float4 *>(a.part + at * D + 64 * i + 4 * (threadIdx.x % 16));
-                v[i][0] += w * o.x, v[i][1] += w * o.y, v[i][2] += w * o.z, v[i][3] += w * o.w;
+            for (int u = 0; u < kJoinAhead; ++u) {
+                const int p = p1 + u * PARTS + l / LANES;
+                const float f = read_from(factor, p < n ? p : 0);
+                if (p < n && f != 0.f)
+                    v[0] += f * x[u].x, v[1] += f * x[u].y, v[2] += f * x[u].z, v[3] += f * x[u].w;
             }
         }
     }
-    const float scale = j.scale();
-    const int token = row / a.group, head = kv_head * a.group + row - token * a.group;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
+    for (int d = 1; d < 64; d *= 2) {
+        weight += read_from(weight, l ^ d);
+        undefined |= read_from(undefined, l ^ d);
+    }
+#pragma unroll
+    for (int d = LANES; d < 64; d *= 2)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            v[i][e] *= scale;
-        Out<E>::store4(a.out, (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D + 64 * i + 4 * (threadIdx.x % 16), v[i]);
-    }
-    if (a.lse && threadIdx.x % 16 == 0)
+            v[e] += read_from(v[e], l ^ d);
+    JoinedRow j;
+    j.m = m, j.w = weight, j.undefined = undefined != 0;
+    const float scale = j.scale();
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        v[e] *= scale;
+    if (l < LANES)
+        Out<E>::store4(a.out, (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D + 4 * l, v);
+    if (a.lse && l == 0)
         a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(j.m, j.weight(), a.scale_log2);
+}
+
+// kJoinRows rows at a time, `blocks` times per (tile, key head); the workgroups of the launch take them in turn until there are
+// no more.  (A workgroup for every piece that there might be took 48 us to find nothing to do for 32768 of them.)
+template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a, int blocks, int workgroups, int most_units)
+{
+    extern __shared__ __align__(16) unsigned char lds_raw[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    for (int unit = blockIdx.x; unit < most_units; unit += workgroups) {
+        Item it;
+        if (!find_item<kJoinThreads, ROWS, KT>(a, unit / blocks / a.Hkv, true, reinterpret_cast<int *>(lds_raw), &it))
+            return;
+        join_row<E, D, ROWS>(a, it, load_seq(a, it.seq), unit / blocks % a.Hkv, unit % blocks * kJoinRows + wave);
+        lds_barrier();
+    }
 }
 
 // ---------------------------------------------------------------- choice of kernels
@@ -952,7 +992,7 @@ struct Launch {
     uint32_t target;
     int min_steps;
     int64_t most_tiles;   // of all sequences, per key head
-    int64_t grid, join_grid, parts, rows_cap;
+    int64_t grid, join_grid, join_units, join_blocks, parts, rows_cap;
     size_t bytes;         // of workspace
 };
 struct Choice {
@@ -978,7 +1018,12 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, int64_
     c.parts = 2 * (int64_t)c.target;
     c.rows_cap = rows < all_rows ? rows : all_rows;
     const int64_t split_tiles = c.most_tiles * s.n_kv_heads < c.target ? c.most_tiles * s.n_kv_heads : c.target;
-    c.join_grid = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * (rows / kJoinRows);
+    c.join_blocks = (c.rows_cap + kJoinRows - 1) / kJoinRows;
+    c.join_units = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * c.join_blocks;
+    c.join_grid = c.join_units < kJoinWorkgroups ? c.join_units : kJoinWorkgroups;
+    // One sequence whose tiles alone are as many as the workgroups wanted has as many steps per workgroup as per tile: no split.
+    if (batch == 1 && (all_rows + rows - 1) / rows * s.n_kv_heads >= c.target)
+        c.join_grid = c.parts = 0;
     c.bytes = (size_t)(c.parts * c.rows_cap) * (s.head_dim + 2) * sizeof(float);
     return c;
 }
@@ -1001,7 +1046,7 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
         c.launch[0] = make_launch(s, batch, T, 16 * c.row_blocks, 0, any, 1024, 8);
         return c;
     }
-    c.launch[0] = make_launch(s, batch, T, kChunkRows, batch > 1 ? 16 : 0, any, 512, 4);
+    c.launch[0] = make_launch(s, batch, T, kChunkRows, batch > 1 ? 16 : 0, any, 512, 8);
     if (batch > 1) {
         c.n = 2;
         c.chunk[1] = false;
@@ -1012,18 +1057,20 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
 
 template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &c, bool few, bool f32, hipStream_t stream)
 {
+    if (c.join_grid == 0)
+        return hipSuccess;
     const dim3 grid((unsigned)c.join_grid), block(kJoinThreads);
     const size_t lds = 16 * sizeof(int);
     if (f32)
-        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, lds, stream, a);
+        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (!few)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, lds, stream, a);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (c.rows == 16)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, lds, stream, a);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (c.rows == 32)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, lds, stream, a);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, lds, stream, a);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     return hipGetLastError();
 }
 
@@ -1089,7 +1136,7 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
 {
     const Choice c = choose(s, batch, T, max_new);
     for (int i = 0; i < c.n; ++i)
-        if (c.launch[i].grid > 0x7fffffff || c.launch[i].join_grid > 0x7fffffff)
+        if (c.launch[i].grid > 0x7fffffff || c.launch[i].join_units > 0x7fffffff - kJoinWorkgroups)
             return hipErrorInvalidValue;
     AttendArgs a;
     a.q = q;

@@ -187,7 +187,8 @@ struct Item {
 };
 
 // The workgroup's `unit`-th (tile, split), or with `of_join` the unit-th tile of the sequences that are split.  Returns
-// false if there is none.  All threads of the workgroup call it; `lds` has room for 2 * NT / 64 + 8 words.
+// false if there is none.  All threads of the workgroup call it, again only behind a barrier; `lds` has room for
+// 2 * NT / 64 + 8 words.
 template <int NT, int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int unit, bool of_join, int *lds, Item *out)
 {
     constexpr int W = NT / 64;
@@ -251,7 +252,7 @@ template <int NT, int ROWS, int KT> __device__ bool find_item(const AttendArgs &
         const int at = unit - (i0 + items_upto - items);
         if (at >= 0 && at < items) {
             lds[2 * W] = b;
-            lds[2 * W + 1] = at;
+            lds[2 * W + 1] = items - 1 - at;  // the last rows, which see the most keys, first
             lds[2 * W + 2] = splits;
             lds[2 * W + 3] = p0 + parts_upto - parts;
         }
