@@ -52,10 +52,10 @@ template <int D> struct ChunkTile {
     static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ v_turn(r)) << 4); }
 };
 
-template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 * NW, 2) void attn_chunk_kernel(AttendArgs a)
+template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 * NW, D == 64 ? 4 : 2) void attn_chunk_kernel(AttendArgs a)
 {
     typedef ChunkTile<D> Tile;
-    constexpr int NT = 64 * NW, ROWS = 32 * NW, PIECES = Tile::kPieces;
+    constexpr int ROWS = 32 * NW, PIECES = Tile::kPieces;
     constexpr int KEYS = kChunkKeys / NW;        // of a tile, that a wave moves
     constexpr int LOADS = KEYS * PIECES / 64;    // copies of K (and of V) for them
     constexpr int ROWS_PER_LOAD = 64 / PIECES;
@@ -64,13 +64,12 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     unsigned char *const lds_k = lds_raw, *const lds_v = lds_raw + kChunkBuffers * Tile::kBytes;
     // of four tiles: which keys exist, and whose V is not finite
     int *const lds_exist = reinterpret_cast<int *>(lds_raw + 2 * kChunkBuffers * Tile::kBytes), *const lds_bad = lds_exist + 4 * kChunkKeys;
-    int *const lds_item = lds_bad + 4 * kChunkKeys;
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), half = l / 32;
     const bool late = wave >= NW / 2;  // one phase behind the others
     const int kv_head = blockIdx.x % a.Hkv;
     Item it;
-    if (!find_item<NT, ROWS, kChunkKeys>(a, blockIdx.x / a.Hkv, false, lds_item, &it))
+    if (!find_item<ROWS, kChunkKeys>(a, blockIdx.x / a.Hkv, false, &it))
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
@@ -124,12 +123,12 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         v_offset[i] = (r - wave * KEYS) * D * 2 + ((load_at ^ Tile::v_turn(r)) << 4);
     }
     constexpr int LOOKS = WIDE ? 1 : LOADS;
-    int block[LOOKS], k_row[LOOKS], v_row[LOOKS];  // WIDE: of the wave's first key, else of the lane's
+    int k_row[LOOKS], v_row[LOOKS];  // WIDE: of the wave's first key, else of the lane's
 #pragma unroll
     for (int i = 0; i < LOOKS; ++i)
         k_row[i] = -1;
     auto first_key = [&](int t) __attribute__((always_inline)) { return keys.tile(step_begin + t) * kChunkKeys; };
-    auto look_up = [&](int j0) __attribute__((always_inline)) {  // the blocks of a tile's keys
+    auto look_up = [&](int j0, int (&block)[LOOKS]) __attribute__((always_inline)) {  // the blocks of a tile's keys
 #pragma unroll
         for (int i = 0; i < LOOKS; ++i) {
             const int e = (j0 + (WIDE ? wave * KEYS : load_row + i * ROWS_PER_LOAD)) >> a.log2_bs;
@@ -138,7 +137,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         }
     };
     // V of a tile, K of tile t behind it, whose first key is j0 and whose blocks have been looked up
-    auto request = [&](int v_buf, int j0, int t, int k_buf) __attribute__((always_inline)) {
+    auto request = [&](int v_buf, int j0, const int (&block)[LOOKS], int t, int k_buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOOKS; ++i) {
             const int j = j0 + (WIDE ? wave * KEYS : load_row + i * ROWS_PER_LOAD);
@@ -190,7 +189,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     };
     // The operands' reads run kAhead products ahead of their use, through both products of a phase.  With the buffers known at
     // compile time their addresses differ by constants: 4 for V (2 with 64 values per head) and 8 (4) for K.
-    constexpr int PV = 4 * (D / 32), QK = 2 * (D / 16), kAhead = 6;
+    constexpr int PV = 4 * (D / 32), QK = 2 * (D / 16), kAhead = D == 64 ? 3 : 6;
     int v_base[D / 32], k_base[D / 16];
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
@@ -311,11 +310,12 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
 
     // first keys of tiles t to t + 3
     int j0 = first_key(0), j1 = first_key(1), j2 = first_key(2), j3 = first_key(3);
-    look_up(j0);
-    request(kChunkBuffers - 1, j0, 0, 0);
-    look_up(j1);
-    request(0, j1, 1, 1);
-    look_up(j2);
+    int block[LOOKS], block0[LOOKS], block1[LOOKS];
+    look_up(j0, block0);
+    look_up(j1, block1);
+    look_up(j2, block);
+    request(kChunkBuffers - 1, j0, block0, 0, 0);
+    request(0, j1, block1, 1, 1);
     arrive(0, j0, 0);
     lds_barrier();
     if (late)
@@ -327,8 +327,8 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         __builtin_amdgcn_sched_barrier(0);
         lds_barrier();
         if (t + 1 < n)
-            request(next, j2, t + 2, after);
-        look_up(j3);
+            request(next, j2, block, t + 2, after);
+        look_up(j3, block);
         if (wave_works)
             softmax(t, j0);
         __builtin_amdgcn_sched_barrier(0);
@@ -406,7 +406,7 @@ template <int D> struct FewTile {
 template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
 {
     typedef FewTile<D> Tile;
-    constexpr int NT = 64 * kFewWaves, ROWS = 16 * RB, PIECES = Tile::kPieces;
+    constexpr int ROWS = 16 * RB, PIECES = Tile::kPieces;
     constexpr int KS = D / 32;                         // products of a block of scores
     constexpr int V_LOADS = kFewKeys * PIECES / 64;    // pieces of V per lane
     constexpr int V_ROWS = 64 / PIECES;                // rows per such load
@@ -416,7 +416,7 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
 
     const int kv_head = blockIdx.x % a.Hkv;
     Item it;
-    if (!find_item<NT, ROWS, kFewKeys>(a, blockIdx.x / a.Hkv, false, reinterpret_cast<int *>(lds_raw), &it))
+    if (!find_item<ROWS, kFewKeys>(a, blockIdx.x / a.Hkv, false, &it))
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
@@ -452,8 +452,6 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
         for (int db = 0; db < D / 16; ++db)
             o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    lds_barrier();  // the words of find_item have been read
-
     uint4 kreg[2][KS], vreg[V_LOADS];
     int block = -1, row_of_key = -1;  // of key l % 32 of a tile: of the one behind the next, of the next
     uint64_t exist_next = 0;
@@ -677,12 +675,11 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     float *const kt = reinterpret_cast<float *>(lds_raw), *const vt = kt + kF32Keys * STRIDE;
     int *const flag = reinterpret_cast<int *>(vt + kF32Keys * STRIDE);  // [32]
     int *const lds_bad = flag + kF32Keys;                               // [32]
-    int *const lds_item = lds_bad + kF32Keys;
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), quarter = l / 16;
     const int kv_head = blockIdx.x % a.Hkv;
     Item it;
-    if (!find_item<NT, ROWS, kF32Keys>(a, blockIdx.x / a.Hkv, false, lds_item, &it))
+    if (!find_item<ROWS, kF32Keys>(a, blockIdx.x / a.Hkv, false, &it))
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
@@ -969,14 +966,12 @@ template <typename E, int D, int ROWS> __device__ __forceinline__ void join_row(
 // no more.  (A workgroup for every piece that there might be took 48 us to find nothing to do for 32768 of them.)
 template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a, int blocks, int workgroups, int most_units)
 {
-    extern __shared__ __align__(16) unsigned char lds_raw[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     for (int unit = blockIdx.x; unit < most_units; unit += workgroups) {
         Item it;
-        if (!find_item<kJoinThreads, ROWS, KT>(a, unit / blocks / a.Hkv, true, reinterpret_cast<int *>(lds_raw), &it))
+        if (!find_item<ROWS, KT>(a, unit / blocks / a.Hkv, true, &it))
             return;
         join_row<E, D, ROWS>(a, it, load_seq(a, it.seq), unit / blocks % a.Hkv, unit % blocks * kJoinRows + wave);
-        lds_barrier();
     }
 }
 
@@ -1037,7 +1032,7 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
     c.row_blocks = 1;
     c.chunk[0] = true;
     if (s.io_dtype == ATTN_DT_F32) {
-        c.launch[0] = make_launch(s, batch, T, kF32Rows, 0, any, 1024, 4);
+        c.launch[0] = make_launch(s, batch, T, kF32Rows, 0, any, 512, 16);
         return c;
     }
     if (rows <= 64) {
@@ -1060,17 +1055,16 @@ template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &
     if (c.join_grid == 0)
         return hipSuccess;
     const dim3 grid((unsigned)c.join_grid), block(kJoinThreads);
-    const size_t lds = 16 * sizeof(int);
     if (f32)
-        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (!few)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (c.rows == 16)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (c.rows == 32)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, lds, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     return hipGetLastError();
 }
 
@@ -1092,7 +1086,7 @@ template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Laun
 {
     hipError_t e;
     if (chunk) {
-        constexpr size_t lds = 2 * kChunkBuffers * (size_t)ChunkTile<D>::kBytes + (8 * kChunkKeys + 2 * kChunkWaves + 8) * sizeof(int);
+        constexpr size_t lds = 2 * kChunkBuffers * (size_t)ChunkTile<D>::kBytes + 8 * kChunkKeys * sizeof(int);
         const bool wide = 1 << a.log2_bs >= kChunkKeys / kChunkWaves;
         e = wide ? lds_limit(attn_chunk_kernel<E, D, kChunkWaves, true>, lds) : lds_limit(attn_chunk_kernel<E, D, kChunkWaves, false>, lds);
         if (e != hipSuccess)
@@ -1110,7 +1104,7 @@ template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Laun
 
 template <int D> hipError_t launch_f32(const AttendArgs &a, const Launch &c, hipStream_t stream)
 {
-    constexpr size_t lds = 2 * (size_t)kF32Keys * (D + 4) * sizeof(float) + (2 * kF32Keys + 2 * kF32Waves + 8) * sizeof(int);
+    constexpr size_t lds = 2 * (size_t)kF32Keys * (D + 4) * sizeof(float) + 2 * kF32Keys * sizeof(int);
     hipLaunchKernelGGL((attn_f32_kernel<D>), dim3((unsigned)c.grid), dim3(64 * kF32Waves), lds, stream, a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : join<float, D>(a, c, false, true, stream);

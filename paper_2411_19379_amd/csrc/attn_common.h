@@ -62,16 +62,28 @@ __device__ __forceinline__ const unsigned char *own_pointer(const void *p)
 
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return a + b < a ? 0xffffffffu : a + b; }
 
-// Inclusive prefix sum over the lanes of a wave.
+#define ATTN_DPP(v, ctrl, row_mask, bound) __builtin_amdgcn_update_dpp(0, (int)(v), (ctrl), (row_mask), 0xF, (bound))
+// Inclusive prefix sums over the lanes of a wave with DPP row shifts and the two row broadcasts.
 __device__ __forceinline__ int wave_scan(int v)
 {
-    const int l = lane_id();
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = read_from(v, l >= d ? l - d : l);
-        v += l >= d ? o : 0;
-    }
+    v += ATTN_DPP(v, 0x111, 0xF, true);   // row_shr:1
+    v += ATTN_DPP(v, 0x112, 0xF, true);   // row_shr:2
+    v += ATTN_DPP(v, 0x114, 0xF, true);   // row_shr:4
+    v += ATTN_DPP(v, 0x118, 0xF, true);   // row_shr:8
+    v += ATTN_DPP(v, 0x142, 0xA, false);  // row_bcast:15 into rows 1 and 3
+    v += ATTN_DPP(v, 0x143, 0xC, false);  // row_bcast:31 into rows 2 and 3
     return v;
+}
+// The sum over the lanes, 2^32 - 1 if it does not fit: saturating sums do not depend on their order.
+__device__ __forceinline__ uint32_t wave_sat_sum(uint32_t v)
+{
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x111, 0xF, true));
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x112, 0xF, true));
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x114, 0xF, true));
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x118, 0xF, true));
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x142, 0xA, false));
+    v = sat_add(v, (uint32_t)ATTN_DPP(v, 0x143, 0xC, false));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 
 // ---------------------------------------------------------------- arguments of attn_attend
@@ -186,88 +198,79 @@ struct Item {
     int part;  // the first partial result of (seq, tile): split s of key head h is part + (tile * n_splits + s) * Hkv + h
 };
 
-// The workgroup's `unit`-th (tile, split), or with `of_join` the unit-th tile of the sequences that are split.  Returns
-// false if there is none.  All threads of the workgroup call it, again only behind a barrier; `lds` has room for
-// 2 * NT / 64 + 8 words.
-template <int NT, int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int unit, bool of_join, int *lds, Item *out)
+// The `unit`-th (tile, split) of the launch, or with `of_join` the unit-th tile of the sequences that are split; false if there is
+// none.  Every wave finds out for itself, four sequences per lane at a time: no barrier, one trip to memory for up to 256
+// sequences.  (With a sequence per thread, sums through LDS and its barriers it was 2.5 us of every workgroup's time.)
+template <int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int unit, bool of_join, Item *out)
 {
-    constexpr int W = NT / 64;
-    const int tid = threadIdx.x, wave = tid / 64, l = lane_id();
-    const bool single = a.batch <= NT;
-    Seq mine = {};
-    uint32_t work = 0;  // steps of all workgroups; saturating sums do not depend on their order
-    for (int b = tid; b < a.batch; b += NT) {
-        const Seq s = load_seq(a, b);
-        if (single)
-            mine = s;
-        if (s.rows > a.min_rows && s.rows <= a.max_rows) {
-            const uint64_t w = (uint64_t)((s.rows + ROWS - 1) / ROWS) * (uint64_t)most_steps<KT>(a, s, ROWS) * (uint64_t)a.Hkv;
-            work = sat_add(work, w > 0xffffffffu ? 0xffffffffu : (uint32_t)w);
-        }
-    }
+    constexpr int PER = 4, ALL = 64 * PER;
+    const int l = lane_id();
+    int tiles[PER], steps[PER];
+    auto load = [&](int b0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        work = sat_add(work, (uint32_t)read_from((int)work, l ^ d));
-    if (l == 0)
-        lds[wave] = (int)work;
-    lds_barrier();
-    work = 0;
-    for (int w = 0; w < W; ++w)
-        work = sat_add(work, (uint32_t)lds[w]);
+        for (int u = 0; u < PER; ++u) {
+            const int b = b0 + l * PER + u;
+            const Seq s = load_seq(a, b < a.batch ? b : a.batch - 1);
+            const bool mine = b < a.batch && s.rows > a.min_rows && s.rows <= a.max_rows;
+            tiles[u] = mine ? (s.rows + ROWS - 1) / ROWS : 0;
+            steps[u] = mine ? most_steps<KT>(a, s, ROWS) : 0;
+        }
+    };
+    uint32_t work = 0;  // steps of all workgroups
+    for (int b0 = 0; b0 < a.batch; b0 += ALL) {
+        load(b0);
+        uint32_t w = 0;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const uint64_t x = (uint64_t)tiles[u] * (uint64_t)steps[u] * (uint64_t)a.Hkv;
+            w = sat_add(w, x > 0xffffffffu ? 0xffffffffu : (uint32_t)x);
+        }
+        work = sat_add(work, wave_sat_sum(w));
+    }
     uint32_t per = work / a.target + (work % a.target != 0);  // steps of a workgroup
     per = per < (uint32_t)a.min_steps ? (uint32_t)a.min_steps : per;
 
     int items_before = 0, parts_before = 0;
-    for (int b0 = 0; b0 < a.batch; b0 += NT) {
-        const int b = b0 + tid;
-        int items = 0, parts = 0, splits = 1;
-        if (b < a.batch) {
-            const Seq s = single ? mine : load_seq(a, b);
-            if (s.rows > a.min_rows && s.rows <= a.max_rows) {
-                const int tiles = (s.rows + ROWS - 1) / ROWS;
-                splits = (int)(((uint32_t)most_steps<KT>(a, s, ROWS) + per - 1) / per);
-                items = tiles * (of_join ? splits > 1 : splits);
-                parts = splits > 1 ? tiles * splits : 0;
-            }
+    for (int b0 = 0; b0 < a.batch; b0 += ALL) {
+        if (a.batch > ALL)
+            load(b0);
+        int splits[PER], items = 0, parts = 0;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            splits[u] = (int)(((uint32_t)steps[u] + per - 1) / per);
+            items += tiles[u] * (of_join ? splits[u] > 1 : splits[u]);
+            parts += splits[u] > 1 ? tiles[u] * splits[u] : 0;
         }
         const int items_upto = wave_scan(items), parts_upto = wave_scan(parts);
-        lds_barrier();  // the words of the pass in front have been read
-        if (l == 63) {
-            lds[wave] = items_upto;
-            lds[W + wave] = parts_upto;
-        }
-        if (tid == 0)
-            lds[2 * W] = -1;
-        lds_barrier();
-        int items_all = 0, i0 = items_before, p0 = parts_before;
-        int parts_all = 0;
-        for (int w = 0; w < W; ++w) {
-            if (w < wave) {
-                i0 += lds[w];
-                p0 += lds[W + w];
+        int at = unit - items_before - (items_upto - items);
+        const uint64_t here = __ballot(at >= 0 && at < items);
+        if (here != 0) {
+            int seq = 0, n_splits = 1, in_seq = 0, of_seq = 1, part = parts_before + parts_upto - parts;
+            bool found = false;
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const int n = tiles[u] * (of_join ? splits[u] > 1 : splits[u]);
+                if (!found && at < n) {
+                    seq = b0 + l * PER + u, n_splits = splits[u], in_seq = at, of_seq = n;
+                    found = true;
+                }
+                if (!found) {
+                    at -= n;
+                    part += splits[u] > 1 ? tiles[u] * splits[u] : 0;
+                }
             }
-            items_all += lds[w];
-            parts_all += lds[W + w];
-        }
-        const int at = unit - (i0 + items_upto - items);
-        if (at >= 0 && at < items) {
-            lds[2 * W] = b;
-            lds[2 * W + 1] = items - 1 - at;  // the last rows, which see the most keys, first
-            lds[2 * W + 2] = splits;
-            lds[2 * W + 3] = p0 + parts_upto - parts;
-        }
-        lds_barrier();
-        if (lds[2 * W] >= 0) {
-            out->seq = lds[2 * W];
-            out->n_splits = lds[2 * W + 2];
-            const int u = lds[2 * W + 1], per_tile = of_join ? 1 : out->n_splits;
-            out->tile = u / per_tile;
-            out->split = u % per_tile;
-            out->part = lds[2 * W + 3];
+            const int owner = __builtin_ctzll(here);
+            out->seq = __builtin_amdgcn_readlane(seq, owner);
+            out->n_splits = __builtin_amdgcn_readlane(n_splits, owner);
+            out->part = __builtin_amdgcn_readlane(part, owner);
+            // the last rows, which see the most keys, first
+            const int left = __builtin_amdgcn_readlane(of_seq, owner) - 1 - __builtin_amdgcn_readlane(in_seq, owner), per_tile = of_join ? 1 : out->n_splits;
+            out->tile = left / per_tile;
+            out->split = left - out->tile * per_tile;
             return true;
         }
-        items_before += items_all;
-        parts_before += parts_all;
+        items_before += __builtin_amdgcn_readlane(items_upto, 63);
+        parts_before += __builtin_amdgcn_readlane(parts_upto, 63);
     }
     return false;
 }
