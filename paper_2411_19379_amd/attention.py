@@ -1,4 +1,4 @@
-"""ctypes binding of the attention layers' operators (`include/attn_cache.h`): argument marshalling only.
+"""Binding of the attention layers' operators (`include/attn_cache.h`): argument marshalling only.
 
     step = assign_blocks(block_size, total_tokens, cu_seqlens, cached_lens, table, free_blocks, n_free)   # once per step
     q = rope_append(q, k, v, step.positions, step.slots, rotary, k_cache, v_cache, copies=step.copies)    # once per layer
@@ -10,7 +10,6 @@ workspace are torch tensors.  There is no CPU fallback: loading raises if the li
 from __future__ import annotations
 
 import ctypes
-import functools
 import math
 import os
 from typing import NamedTuple, Optional
@@ -84,71 +83,22 @@ def attn_workspace_bytes(shape: AttnShape, batch: int, total_tokens: int, max_ne
     return n.value
 
 
-# A decode step of one layer is a few microseconds of GPU work and each line here costs a tenth of one: what follows from sizes
-# alone is kept, and tensors are checked in one expression each.
-_DTYPES = {torch.float32: ATTN_DT_F32, torch.bfloat16: ATTN_DT_BF16, torch.float16: ATTN_DT_F16}
-_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
-# the raw handle of a GPU's current stream, without the object that torch.cuda.current_stream makes where there is a way
-_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_binding = None
 
 
-@functools.lru_cache(maxsize=256)
-def _shape_of(n_q_heads, n_kv_heads, head_dim, block_size, dtype):
-    """The address of the shape."""
-    if dtype not in _DTYPES:
-        raise ValueError(f"expected float32, bfloat16 or float16, got {dtype}")
-    return ctypes.byref(AttnShape(n_q_heads, n_kv_heads, head_dim, block_size, _DTYPES[dtype]))
-
-
-@functools.lru_cache(maxsize=4096)
-def _workspace_of(n_q_heads, n_kv_heads, head_dim, block_size, dtype, batch, total_tokens, max_new):
-    shape = AttnShape(n_q_heads, n_kv_heads, head_dim, block_size, _DTYPES[dtype])
-    return attn_workspace_bytes(shape, batch, total_tokens, max_new)
-
-
-def _refuse(name, t, shape, dtype, index):
-    raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}, "
-                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
-
-
-def _ints(name, t, n, index):
-    """The address of n contiguous int32 values on GPU `index` (n None: any number)."""
-    if t.dtype is not _I32 or t.get_device() != index or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
-        _refuse(name, t, (n,), _I32, index)
-    return t.data_ptr()
-
-
-def _rows(name, t, n, index):
-    """The address and the width of n contiguous rows of int32 values."""
-    have = t.shape
-    if t.dtype is not _I32 or t.get_device() != index or len(have) != 2 or have[0] != n or not t.is_contiguous():
-        _refuse(name, t, (n, "any"), _I32, index)
-    return t.data_ptr(), have[1]
-
-
-def _tensor(name, t, shape, dtype, index):
-    """The address of a contiguous tensor."""
-    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
-        _refuse(name, t, shape, dtype, index)
-    return t.data_ptr()
-
-
-def _heads(name, t, shape, dtype, index):
-    """[tokens, heads, head_dim] whose heads are contiguous; returns the address and the elements between tokens."""
-    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
-        _refuse(name, t, shape, dtype, index)
-    tokens, heads, dim = t.stride()
-    if (dim != 1 and shape[2] > 1) or (heads != shape[2] and shape[1] > 1):
-        raise ValueError(f"{name}: the heads of a token must be contiguous, got strides {t.stride()}")
-    return t.data_ptr(), (tokens if shape[0] > 1 else shape[1] * shape[2])
-
-
-def _device(t):
-    """The index of the current GPU, which the tensor has to be on."""
-    index = t.get_device()
-    if index < 0 or index != torch.cuda.current_device():
-        raise ValueError(f"expected tensors on the current CUDA device, got {t.device}")
-    return index
+def _native():
+    """The compiled binding (csrc/attn_binding.cpp), which checks tensors and allocates outputs; raises if it is not built."""
+    global _binding
+    if _binding is None:
+        load_library()
+        try:
+            from . import _attn_binding
+        except ImportError as e:
+            raise ImportError(f"the attention binding is not built or does not fit this torch ({e}): "
+                              "run `python -m paper_2411_19379_amd.build`") from e
+        _attn_binding.set_error_class(AttnError)
+        _binding = _attn_binding
+    return _binding
 
 
 class Step(NamedTuple):
@@ -164,19 +114,8 @@ def assign_blocks(block_size: int, total_tokens: int, cu_seqlens, cached_lens, t
                   shared_tail=None, in_place: bool = False) -> Step:
     """Blocks, slots and positions of the new tokens of a batch.  `n_free` is a device int32 tensor of one value; the
     next step's is `counts[:1]` of this one.  `in_place` extends the rows of `table`, else they are written to a new one."""
-    dev = _device(cu_seqlens)
-    batch = cu_seqlens.numel() - 1
-    tab, width = _rows("table", table, batch, dev)
-    out = table if in_place else torch.empty_like(table)
-    slots = torch.empty((total_tokens,), dtype=_I64, device=table.device)
-    positions, copies, counts = table.new_empty((total_tokens,)), table.new_empty((batch, 4)), table.new_empty((2,))
-    _check(load_library().attn_assign_blocks(
-        batch, block_size, width, total_tokens, _ints("cu_seqlens", cu_seqlens, batch + 1, dev),
-        _ints("cached_lens", cached_lens, batch, dev),
-        None if shared_tail is None else _ints("shared_tail", shared_tail, batch, dev), tab, out.data_ptr(),
-        _ints("free_blocks", free_blocks, None, dev), _ints("n_free", n_free, 1, dev), free_blocks.numel(), slots.data_ptr(),
-        positions.data_ptr(), copies.data_ptr(), counts.data_ptr(), _stream(dev)))
-    return Step(out, slots, positions, copies, counts)
+    return Step._make((_binding or _native()).assign_blocks(block_size, total_tokens, cu_seqlens, cached_lens, table, free_blocks,
+                                                            n_free, shared_tail, in_place))
 
 
 def rotary_table(max_positions: int, rotary_dim: int, base: float = 10000.0, *, linear: float = 1.0,
@@ -199,43 +138,11 @@ def rotary_table(max_positions: int, rotary_dim: int, base: float = 10000.0, *, 
     return torch.stack([angle.cos() * size, angle.sin() * size], 1).float().contiguous().to(device)
 
 
-def _caches(k_cache, v_cache, dtype, index):
-    """The caches' extents and addresses."""
-    extents = k_cache.shape
-    if len(extents) != 4:
-        raise ValueError(f"k_cache: expected [n_blocks, n_kv_heads, block_size, head_dim], got {tuple(extents)}")
-    return extents, _tensor("k_cache", k_cache, extents, dtype, index), _tensor("v_cache", v_cache, extents, dtype, index)
-
-
 def rope_append(q, k, v, positions, slots, rotary, k_cache, v_cache, *, interleaved: bool = False, copies=None, q_out=None):
     """Rotary positions on q and k, k and v into the cache; returns the turned q [tokens, n_q_heads, head_dim].
     q, k and v may be parts of one projection's rows.  `rotary` is a `rotary_table` or None, `copies` comes from
     `assign_blocks` where sequences share their tails."""
-    dev, dtype = _device(q), q.dtype
-    T, hq = q.shape[:2]
-    (n_blocks, hkv, bs, d), k_to, v_to = _caches(k_cache, v_cache, dtype, dev)
-    shape = _shape_of(hq, hkv, d, bs, dtype)
-    q_shape, kv_shape = (T, hq, d), (T, hkv, d)
-    qp, qs = _heads("q", q, q_shape, dtype, dev)
-    kp, ks = _heads("k", k, kv_shape, dtype, dev)
-    vp, vs = _heads("v", v, kv_shape, dtype, dev)
-    pos = table = copy = None
-    most = rot = batch = 0
-    if rotary is not None:
-        pos = _ints("positions", positions, T, dev)
-        if rotary.dim() != 3 or rotary.shape[1] != 2:
-            raise ValueError(f"rotary: expected [positions, 2, rotary_dim / 2], got {tuple(rotary.shape)}")
-        most, _, rot = rotary.shape
-        table, rot = _tensor("rotary", rotary, (most, 2, rot), _F32, dev), 2 * rot
-    if copies is not None:
-        batch = copies.shape[0]
-        copy = _tensor("copies", copies, (batch, 4), _I32, dev)
-    if q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    _check(load_library().attn_rope_append(
-        shape, T, batch, n_blocks, qp, qs, kp, ks, vp, vs, pos, _tensor("slots", slots, (T,), _I64, dev), table, most, rot,
-        int(interleaved), copy, _tensor("q_out", q_out, q_shape, dtype, dev), k_to, v_to, _stream(dev)))
-    return q_out
+    return (_binding or _native()).rope_append(q, k, v, positions, slots, rotary, k_cache, v_cache, interleaved, copies, q_out)
 
 
 def attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, *, scale: Optional[float] = None, window: int = 0,
@@ -243,22 +150,5 @@ def attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, *, scale: Option
     """Attention of the new tokens over the cache.  Returns out [tokens, n_q_heads, head_dim], with `return_lse` also the
     log of the sum of exponentials [tokens, n_q_heads].  `scale` is 1 / sqrt(head_dim) if not given; `max_new`, the largest
     number of new tokens of any sequence, picks the faster kernel (0: not known)."""
-    dev, dtype = _device(q), q.dtype
-    T, hq = q.shape[:2]
-    (n_blocks, hkv, bs, d), kp, vp = _caches(k_cache, v_cache, dtype, dev)
-    shape = _shape_of(hq, hkv, d, bs, dtype)
-    batch = cu_seqlens.numel() - 1
-    q_shape = (T, hq, d)
-    qp, qs = _heads("q", q, q_shape, dtype, dev)
-    tab, width = _rows("table", table, batch, dev)
-    if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    op, os_ = _heads("out", out, q_shape, dtype, dev)
-    lse = torch.empty((T, hq), dtype=_F32, device=q.device) if return_lse else None
-    need = _workspace_of(hq, hkv, d, bs, dtype, batch, T, max_new)
-    ws = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
-    _check(load_library().attn_attend(
-        shape, batch, T, n_blocks, width, qp, qs, kp, vp, tab, _ints("cu_seqlens", cu_seqlens, batch + 1, dev),
-        _ints("cached_lens", cached_lens, batch, dev), 1.0 / math.sqrt(d) if scale is None else scale, window, sinks, max_new,
-        op, os_, lse.data_ptr() if return_lse else None, ws.data_ptr() if need else None, need, _stream(dev)))
-    return (out, lse) if return_lse else out
+    return (_binding or _native()).attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, scale, window, sinks, max_new, out,
+                                          return_lse)

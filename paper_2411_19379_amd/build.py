@@ -55,6 +55,29 @@ def build_attention(verbose: bool = False) -> str:
     return ATTN_LIB_PATH
 
 
+ATTN_BINDING_PATH = os.path.join(_PKG, "_attn_binding.so")
+
+
+def build_attention_binding(verbose: bool = False) -> str:
+    """The binding of these operators to torch tensors: host code over the C ABI, linked against the library beside it."""
+    import sysconfig
+
+    import torch
+
+    base = os.path.dirname(torch.__file__)
+    include, lib = os.path.join(base, "include"), os.path.join(base, "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", "/opt/rocm/include",
+           "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(_ROOT, "include"),
+           "-o", ATTN_BINDING_PATH, os.path.join(CSRC, "attn_binding.cpp"), "-L", _PKG, "-l:libattn_cache.so", "-Wl,-rpath,$ORIGIN",
+           "-L", lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return ATTN_BINDING_PATH
+
+
 PEAK_PROBE_PATH = os.path.join(_PKG, "peak_probe")
 
 
@@ -72,4 +95,5 @@ if __name__ == "__main__":
     build_library(verbose=True)
     build_prefix_cache(verbose=True)
     build_attention(verbose=True)
+    build_attention_binding(verbose=True)
     build_peak_probe(verbose=True)
