@@ -199,11 +199,11 @@ struct Item {
 };
 
 // The `unit`-th (tile, split) of the launch, or with `of_join` the unit-th tile of the sequences that are split; false if there is
-// none.  Every wave finds out for itself, four sequences per lane at a time: no barrier, one trip to memory for up to 256
+// none.  Every wave finds out for itself, PER sequences per lane at a time: no barrier, one trip to memory for up to 64 PER
 // sequences.  (With a sequence per thread, sums through LDS and its barriers it was 2.5 us of every workgroup's time.)
-template <int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int unit, bool of_join, Item *out)
+template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(const AttendArgs &a, int unit, bool of_join, Item *out)
 {
-    constexpr int PER = 4, ALL = 64 * PER;
+    constexpr int ALL = 64 * PER;
     const int l = lane_id();
     int tiles[PER], steps[PER];
     auto load = [&](int b0) __attribute__((always_inline)) {
@@ -273,6 +273,10 @@ template <int ROWS, int KT> __device__ bool find_item(const AttendArgs &a, int u
         parts_before += __builtin_amdgcn_readlane(parts_upto, 63);
     }
     return false;
+}
+template <int ROWS, int KT> __device__ __forceinline__ bool find_item(const AttendArgs &a, int unit, bool of_join, Item *out)
+{
+    return a.batch <= 64 ? find_among<1, ROWS, KT>(a, unit, of_join, out) : find_among<4, ROWS, KT>(a, unit, of_join, out);
 }
 __device__ __forceinline__ int part_of(const AttendArgs &a, const Item &it, int kv_head, int split)
 {

@@ -159,44 +159,39 @@ struct RopeArgs {
 };
 
 // 8 neighbouring values
-template <typename IO> struct Eight;
+template <typename E> struct Eight {
+    typedef uint16_t type;
+    static __device__ __forceinline__ void read(const uint16_t *p, float *v)
+    {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
+        v[0] = E::lo(a.x), v[1] = E::hi(a.x), v[2] = E::lo(a.y), v[3] = E::hi(a.y);
+        v[4] = E::lo(a.z), v[5] = E::hi(a.z), v[6] = E::lo(a.w), v[7] = E::hi(a.w);
+    }
+    static __device__ __forceinline__ void write(uint16_t *p, const float *v)
+    {
+        *reinterpret_cast<uint4 *>(p) = make_uint4(E::pack(v[0], v[1]), E::pack(v[2], v[3]), E::pack(v[4], v[5]), E::pack(v[6], v[7]));
+    }
+    static __device__ __forceinline__ void copy(const uint16_t *from, uint16_t *to) { *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from); }
+};
 template <> struct Eight<float> {
     typedef float type;
-    uint4 a, b;
-    __device__ __forceinline__ void load(const float *p) { a = reinterpret_cast<const uint4 *>(p)[0], b = reinterpret_cast<const uint4 *>(p)[1]; }
-    __device__ __forceinline__ void store(float *p) const { reinterpret_cast<uint4 *>(p)[0] = a, reinterpret_cast<uint4 *>(p)[1] = b; }
-    __device__ __forceinline__ void unpack(float *v) const
+    static __device__ __forceinline__ void read(const float *p, float *v)
     {
-        const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = __uint_as_float(w[e]);
+        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
     }
-    __device__ __forceinline__ void pack(const float *v)
+    static __device__ __forceinline__ void write(float *p, const float *v)
     {
-        a = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        b = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
-};
-template <typename E> struct Eight16 {
-    typedef uint16_t type;
-    uint4 a;
-    __device__ __forceinline__ void load(const uint16_t *p) { a = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void store(uint16_t *p) const { *reinterpret_cast<uint4 *>(p) = a; }
-    __device__ __forceinline__ void unpack(float *v) const
+    static __device__ __forceinline__ void copy(const float *from, float *to)
     {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[2 * e] = E::lo(w[e]), v[2 * e + 1] = E::hi(w[e]);
-    }
-    __device__ __forceinline__ void pack(const float *v)
-    {
-        a = make_uint4(E::pack(v[0], v[1]), E::pack(v[2], v[3]), E::pack(v[4], v[5]), E::pack(v[6], v[7]));
+        const uint4 a = reinterpret_cast<const uint4 *>(from)[0], b = reinterpret_cast<const uint4 *>(from)[1];
+        reinterpret_cast<uint4 *>(to)[0] = a;
+        reinterpret_cast<uint4 *>(to)[1] = b;
     }
 };
-template <> struct Eight<Bf16> : Eight16<Bf16> {};
-template <> struct Eight<F16> : Eight16<F16> {};
 
 template <typename E> __global__ __launch_bounds__(kRopeThreads) void attn_rope_kernel(RopeArgs a)
 {
@@ -204,19 +199,18 @@ template <typename E> __global__ __launch_bounds__(kRopeThreads) void attn_rope_
     typedef typename V::type elem;
     const int bs = 1 << a.log2_bs;
     if ((int64_t)blockIdx.x >= a.token_workgroups) {
-        // the shared tail blocks: one workgroup per sequence
-        const int32_t *c = a.copies + (int64_t)(blockIdx.x - a.token_workgroups) * 4;
+        // the shared tail blocks: a workgroup per sequence, cache and head, whose rows are contiguous (a workgroup per sequence
+        // took 15 us for 15 rows of 4 heads)
+        const int unit = (int)(blockIdx.x - a.token_workgroups), of_seq = 2 * a.Hkv, seq = unit / of_seq, h = (unit - seq * of_seq) >> 1;
+        const int32_t *c = a.copies + (int64_t)seq * 4;
         const int from = c[0], to = c[1], rows = c[2] < bs ? c[2] : bs;
         if ((uint32_t)from >= (uint32_t)a.n_blocks || (uint32_t)to >= (uint32_t)a.n_blocks)
             return;
-        const int run = rows * (a.D / 8);  // of a head, contiguous
-        for (int i = threadIdx.x; i < 2 * a.Hkv * run; i += kRopeThreads) {
-            elem *cache = static_cast<elem *>(i < a.Hkv * run ? a.k_cache : a.v_cache);
-            const int h = i / run % a.Hkv, at = i % run;
-            V v;
-            v.load(cache + ((((int64_t)from * a.Hkv + h) << a.log2_bs) * a.D + at * 8));
-            v.store(cache + ((((int64_t)to * a.Hkv + h) << a.log2_bs) * a.D + at * 8));
-        }
+        elem *const cache = static_cast<elem *>(unit & 1 ? a.v_cache : a.k_cache);
+        const elem *const src = cache + (((int64_t)from * a.Hkv + h) << a.log2_bs) * a.D;
+        elem *const dst = cache + (((int64_t)to * a.Hkv + h) << a.log2_bs) * a.D;
+        for (int i = threadIdx.x; i < rows * (a.D / 8); i += kRopeThreads)
+            V::copy(src + i * 8, dst + i * 8);
         return;
     }
     const int64_t at = (int64_t)blockIdx.x * kRopeThreads + threadIdx.x;
@@ -246,54 +240,38 @@ template <typename E> __global__ __launch_bounds__(kRopeThreads) void attn_rope_
     }
     if (of_v || part >= a.turned_units) {
         const int d = of_v ? part * 8 : a.rot + (part - a.turned_units) * 8;
-        V v;
-        v.load(src + d);
-        v.store(dst + d);
+        V::copy(src + d, dst + d);
         return;
     }
     const int d0 = a.interleaved ? part * 16 : part * 8, d1 = a.interleaved ? d0 + 8 : d0 + a.rot / 2;
-    V lo, hi;
-    lo.load(src + d0);
-    hi.load(src + d1);
     const int pos = a.positions[t];
+    const bool known = (uint32_t)pos < (uint32_t)a.max_positions;
     float c[8], s[8], x[8], y[8];
-    if ((uint32_t)pos < (uint32_t)a.max_positions) {
-        const float *row = a.rotary + (int64_t)pos * a.rot + part * 8;
-        Eight<float> w;
-        w.load(row);
-        w.unpack(c);
-        w.load(row + a.rot / 2);
-        w.unpack(s);
-    } else {
+    const float *const row = a.rotary + (int64_t)(known ? pos : 0) * a.rot + part * 8;
+    Eight<float>::read(row, c);
+    Eight<float>::read(row + a.rot / 2, s);
+    V::read(src + d0, x);
+    V::read(src + d1, y);
+    const float nan_else_0 = known ? 0.f : NAN;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            c[e] = s[e] = NAN;
+    for (int e = 0; e < 8; ++e)
+        c[e] += nan_else_0, s[e] += nan_else_0;
+    float u[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // interleaved: x and y hold pairs 0..3 and 4..7
+        const float first = a.interleaved ? (e < 4 ? x : y)[2 * (e % 4)] : x[e], second = a.interleaved ? (e < 4 ? x : y)[2 * (e % 4) + 1] : y[e];
+        u[e] = first * c[e] - second * s[e];
+        v[e] = second * c[e] + first * s[e];
     }
-    lo.unpack(x);
-    hi.unpack(y);
-    if (a.interleaved) {  // x and y hold pairs 0..3 and 4..7
-        float u[8], v[8];
+    float p[8], q[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            u[2 * e] = x[2 * e] * c[e] - x[2 * e + 1] * s[e];
-            u[2 * e + 1] = x[2 * e + 1] * c[e] + x[2 * e] * s[e];
-            v[2 * e] = y[2 * e] * c[4 + e] - y[2 * e + 1] * s[4 + e];
-            v[2 * e + 1] = y[2 * e + 1] * c[4 + e] + y[2 * e] * s[4 + e];
-        }
-        lo.pack(u);
-        hi.pack(v);
-    } else {
-        float u[8], v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            u[e] = x[e] * c[e] - y[e] * s[e];
-            v[e] = y[e] * c[e] + x[e] * s[e];
-        }
-        lo.pack(u);
-        hi.pack(v);
+    for (int e = 0; e < 8; ++e) {
+        p[e] = a.interleaved ? (e % 2 ? v : u)[e / 2] : u[e];
+        q[e] = a.interleaved ? (e % 2 ? v : u)[4 + e / 2] : v[e];
     }
-    lo.store(dst + d0);
-    hi.store(dst + d1);
+    V::write(dst + d0, p);
+    V::write(dst + d1, q);
 }
 
 }  // namespace
@@ -362,7 +340,7 @@ hipError_t launch_attn_rope(const attn_shape_t &s, int64_t T, int batch, int n_b
     a.token_units = (a.Hq + a.Hkv) * a.head_units + a.Hkv * (a.D / 8);
     a.interleaved = interleaved;
     a.token_workgroups = (T * a.token_units + kRopeThreads - 1) / kRopeThreads;
-    const int64_t n = a.token_workgroups + (copies ? batch : 0);
+    const int64_t n = a.token_workgroups + (copies ? (int64_t)batch * 2 * a.Hkv : 0);
     if (n == 0)
         return hipSuccess;
     if (n > 0x7fffffff)
