@@ -76,7 +76,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     const KeyRange keys = key_range<kChunkKeys>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits);
     const int n = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits) - step_begin;
-    const int end = keys.pos1 + 1;  // no row of the workgroup sees a key behind it
+    const int end = keys.end;
 
     // this lane's row
     const int row = r0 + 32 * wave + l % 32;
@@ -422,7 +422,7 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
     const int r0 = it.tile * ROWS;
     const KeyRange keys = key_range<kFewKeys>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
-    const int end = keys.pos1 + 1;
+    const int end = keys.end;
 
     int pos[RB], token[RB], head[RB];
     bool row_works[RB];
@@ -661,8 +661,8 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
 }
 
 // ================================================================ fp32
-// 16 rows per wave, 64 per workgroup, keys in tiles of 32 through LDS; products on the fp32 matrix instructions, which bound
-// it (a sixteenth of the 16-bit rate).
+// 16 rows per wave, 64 per workgroup, keys in tiles of 32 through LDS in two buffers; products on the fp32 matrix instructions,
+// which bound it (a sixteenth of the 16-bit rate).
 constexpr int kF32Keys = 32;
 constexpr int kF32Waves = 4;
 
@@ -672,9 +672,9 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     constexpr int PIECES = D / 4, LOADS = kF32Keys * PIECES / NT, ROWS_PER_LOAD = NT / PIECES;
     constexpr int STRIDE = D + 4;  // floats; rows four apart start 16 banks apart
     extern __shared__ __align__(16) unsigned char lds_raw[];
-    float *const kt = reinterpret_cast<float *>(lds_raw), *const vt = kt + kF32Keys * STRIDE;
-    int *const flag = reinterpret_cast<int *>(vt + kF32Keys * STRIDE);  // [32]
-    int *const lds_bad = flag + kF32Keys;                               // [32]
+    constexpr int TILE = kF32Keys * STRIDE;
+    float *const lds_k = reinterpret_cast<float *>(lds_raw), *const lds_v = lds_k + 2 * TILE;
+    int *const lds_flag = reinterpret_cast<int *>(lds_v + 2 * TILE);  // [2][32]: bit 0 the key exists, bit 1 its V is not finite
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), l = lane_id(), quarter = l / 16;
     const int kv_head = blockIdx.x % a.Hkv;
@@ -685,18 +685,18 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     const int r0 = it.tile * ROWS;
     const KeyRange keys = key_range<kF32Keys>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
-    const int end = keys.pos1 + 1;
+    const int end = keys.end;
 
     const int row = r0 + 16 * wave + l % 16;
     const bool wave_works = r0 + 16 * wave < s.rows, row_works = row < s.rows;
     const int token = row_works ? row / a.group : 0, head = kv_head * a.group + (row_works ? row - token * a.group : 0);
     const int pos = s.cached + token;
-    float4 qf[D / 16];
+    f32x4 qf[D / 16];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
-        qf[ks] = make_float4(0.f, 0.f, 0.f, 0.f);
+        qf[ks] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (row_works)
-            qf[ks] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + (int64_t)(s.start + token) * a.q_stride +
+            qf[ks] = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.q) + (int64_t)(s.start + token) * a.q_stride +
                                                        (int64_t)head * D + ks * 16 + 4 * quarter);
     }
     f32x4 o[D / 16];
@@ -706,29 +706,28 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     float m = -INFINITY, lsum = 0.f;
     bool seen = false;
 
-    const int load_row = tid / PIECES, load_piece = tid % PIECES;
-    float4 kreg[LOADS], vreg[LOADS];
-    int block[LOADS];
-    int there = 0;
+    // as in the kernel for chunks: a key that does not exist is read from the cache's first row, as V it is cleared
+    const int load_row = tid / PIECES, load_piece = tid % PIECES, bs_mask = (1 << a.log2_bs) - 1;
+    const int32_t *const table = a.table + (int64_t)it.seq * a.max_blocks;
+    f32x4 kreg[LOADS], vreg[LOADS];  // (of float4 one would be kept in memory)
+    int block[LOADS], k_row[LOADS];
     auto look_up = [&](int step) __attribute__((always_inline)) {
-        const int j0 = keys.tile(step) * kF32Keys;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-            block[i] = step < step_end ? table_entry(a, it.seq, j0 + load_row + i * ROWS_PER_LOAD, end) : -1;
-    };
-    auto request = [&](int step) __attribute__((always_inline)) {
-        const int j0 = keys.tile(step) * kF32Keys;
-        there = 0;
+        const int j0 = keys.tile(step) * kF32Keys + load_row;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int r = cache_row(a, block[i], kv_head, j0 + load_row + i * ROWS_PER_LOAD);
-            kreg[i] = vreg[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (r >= 0) {
-                const int64_t at = (int64_t)r * D + load_piece * 4;
-                kreg[i] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.k_cache) + at);
-                vreg[i] = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.v_cache) + at);
-                there |= 1 << i;
-            }
+            const int e = (j0 + i * ROWS_PER_LOAD) >> a.log2_bs;
+            block[i] = table[(uint32_t)e < (uint32_t)a.max_blocks ? e : a.max_blocks - 1];
+        }
+    };
+    auto request = [&](int step) __attribute__((always_inline)) {
+        const int j0 = keys.tile(step) * kF32Keys + load_row;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int j = j0 + i * ROWS_PER_LOAD;
+            k_row[i] = j < end && (uint32_t)block[i] < (uint32_t)a.n_blocks ? ((block[i] * a.Hkv + kv_head) << a.log2_bs) + (j & bs_mask) : -1;
+            const int64_t at = (int64_t)(k_row[i] < 0 ? 0 : k_row[i]) * D + load_piece * 4;
+            kreg[i] = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.k_cache) + at);
+            vreg[i] = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.v_cache) + at);
         }
     };
     if (step_begin < step_end) {
@@ -740,45 +739,53 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     for (int step = step_begin; step < step_end; ++step) {
         const int j0 = keys.tile(step) * kF32Keys;
         const bool part_seen = !seen_tiles.all(j0);
-        lds_barrier();  // the tile in front has been read
-        if (tid < kF32Keys)
-            lds_bad[tid] = 0;
-        lds_barrier();
+        float *const kt = lds_k + (step & 1) * TILE, *const vt = lds_v + (step & 1) * TILE;
+        int *const flag = lds_flag + (step & 1) * kF32Keys;
+        bool missing = false;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            missing = missing || k_row[i] < 0;
+        const bool clear = part_seen || __any(missing);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int r = load_row + i * ROWS_PER_LOAD;
-            if (part_seen) {
-                const bool bx = not_finite(vreg[i].x), by = not_finite(vreg[i].y), bz = not_finite(vreg[i].z), bw = not_finite(vreg[i].w);
-                vreg[i] = make_float4(bx ? 0.f : vreg[i].x, by ? 0.f : vreg[i].y, bz ? 0.f : vreg[i].z, bw ? 0.f : vreg[i].w);
-                if (bx || by || bz || bw)
-                    lds_bad[r] = 1;
+            int bad = 0;
+            if (clear) {
+                const bool there = k_row[i] >= 0;
+                uint4 v = __builtin_bit_cast(uint4, vreg[i]);
+                const uint32_t all = part_seen ? 0x7f800000u : 0xffffffffu;  // what no value's exponent equals where nothing is dropped
+                const bool dx = (v.x & 0x7f800000u) == all, dy = (v.y & 0x7f800000u) == all, dz = (v.z & 0x7f800000u) == all, dw = (v.w & 0x7f800000u) == all;
+                const bool mine = there && (dx || dy || dz || dw);
+                v = make_uint4(there && !dx ? v.x : 0u, there && !dy ? v.y : 0u, there && !dz ? v.z : 0u, there && !dw ? v.w : 0u);
+                vreg[i] = __builtin_bit_cast(f32x4, v);
+                bad = (__ballot(mine) >> (l / PIECES * PIECES) & ((1ull << PIECES) - 1)) != 0 ? 2 : 0;
             }
-            *reinterpret_cast<float4 *>(kt + r * STRIDE + load_piece * 4) = kreg[i];
-            *reinterpret_cast<float4 *>(vt + r * STRIDE + load_piece * 4) = vreg[i];
-            if (load_piece == 0)
-                flag[r] = there >> i & 1;
+            *reinterpret_cast<f32x4 *>(kt + r * STRIDE + load_piece * 4) = kreg[i];
+            *reinterpret_cast<f32x4 *>(vt + r * STRIDE + load_piece * 4) = vreg[i];
+            flag[r] = (k_row[i] >= 0 ? 1 : 0) | bad;  // the same from all lanes of the row
         }
         if (step + 1 < step_end) {
             request(step + 1);
             look_up(step + 2);
         }
-        lds_barrier();
+        lds_barrier();  // also behind the reads of the buffer that the next tile goes to
         if (!wave_works)
             continue;
-        f32x4 st[2];
+        f32x4 st[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            st[kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int ks = 0; ks < D / 16; ++ks) {
+            f32x4 kf[2];
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const float4 kf = *reinterpret_cast<const float4 *>(kt + (kb * 16 + l % 16) * STRIDE + ks * 16 + 4 * quarter);
-                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.x, qf[ks].x, st[kb], 0, 0, 0);
-                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.y, qf[ks].y, st[kb], 0, 0, 0);
-                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.z, qf[ks].z, st[kb], 0, 0, 0);
-                st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf.w, qf[ks].w, st[kb], 0, 0, 0);
-            }
+            for (int kb = 0; kb < 2; ++kb)
+                kf[kb] = *reinterpret_cast<const f32x4 *>(kt + (kb * 16 + l % 16) * STRIDE + ks * 16 + 4 * quarter);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)  // two sums in turn: a product waits for the one in front of it
+                    st[kb] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kb][e], qf[ks][e], st[kb], 0, 0, 0);
         }
-        const uint32_t exist = (uint32_t)__ballot(flag[l % 32] != 0), bad = (uint32_t)__ballot(lds_bad[l % 32] != 0);
+        const int f = flag[l % 32];
+        const uint32_t exist = (uint32_t)__ballot((f & 1) != 0), bad = (uint32_t)__ballot((f & 2) != 0);
         const bool partly = part_seen || exist != 0xffffffffu;
         if (partly) {
             const uint32_t keys_seen = (uint32_t)seen_keys(a, pos, j0, exist), mine = keys_seen >> (4 * quarter);
@@ -825,7 +832,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
                     o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(kb * 16 + 4 * quarter + r) * STRIDE + db * 16 + l % 16], st[kb][r], o[db], 0, 0, 0);
         for (uint32_t left = bad; left != 0; left &= left - 1) {
             const int key = __builtin_ctz(left), e_of = 4 * (key / 16) + key % 4, from = key % 16 / 4;
-            const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
+            const int e = (j0 + key) >> a.log2_bs, cr = cache_row(a, j0 + key < end && e < a.max_blocks ? table[e] : -1, kv_head, j0 + key);
             const float *v_row = static_cast<const float *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
             float p = 0.f;
 #pragma unroll
@@ -1038,21 +1045,32 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
     if (rows <= 64) {
         c.chunk[0] = false;
         c.row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-        c.launch[0] = make_launch(s, batch, T, 16 * c.row_blocks, 0, any, 1024, 8);
+        c.launch[0] = make_launch(s, batch, T, 16 * c.row_blocks, 0, any, 768, 4);
         return c;
     }
     c.launch[0] = make_launch(s, batch, T, kChunkRows, batch > 1 ? 16 : 0, any, 512, 8);
     if (batch > 1) {
         c.n = 2;
         c.chunk[1] = false;
-        c.launch[1] = make_launch(s, batch, T, 16, 0, 16, 1024, 8);
+        c.launch[1] = make_launch(s, batch, T, 16, 0, 16, 768, 4);
     }
     return c;
 }
 
+// The most steps of KT keys that a tile of `rows` rows can have in a table of this width: no more than min_steps are never split.
+template <int KT> bool may_split(const AttendArgs &a, const Launch &c)
+{
+    int64_t steps = ((((int64_t)a.max_blocks << a.log2_bs) + KT - 1) / KT);
+    if (a.window > 0) {
+        const int64_t seen = ((int64_t)a.window + c.rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
+        steps = seen < steps ? seen : steps;
+    }
+    return steps > c.min_steps;
+}
+
 template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &c, bool few, bool f32, hipStream_t stream)
 {
-    if (c.join_grid == 0)
+    if (c.join_grid == 0 || !(f32 ? may_split<kF32Keys>(a, c) : few ? may_split<kFewKeys>(a, c) : may_split<kChunkKeys>(a, c)))
         return hipSuccess;
     const dim3 grid((unsigned)c.join_grid), block(kJoinThreads);
     if (f32)
@@ -1104,7 +1122,10 @@ template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Laun
 
 template <int D> hipError_t launch_f32(const AttendArgs &a, const Launch &c, hipStream_t stream)
 {
-    constexpr size_t lds = 2 * (size_t)kF32Keys * (D + 4) * sizeof(float) + 2 * kF32Keys * sizeof(int);
+    constexpr size_t lds = 4 * (size_t)kF32Keys * (D + 4) * sizeof(float) + 2 * kF32Keys * sizeof(int);
+    const hipError_t limit = lds_limit(attn_f32_kernel<D>, lds);
+    if (limit != hipSuccess)
+        return limit;
     hipLaunchKernelGGL((attn_f32_kernel<D>), dim3((unsigned)c.grid), dim3(64 * kF32Waves), lds, stream, a);
     const hipError_t e = hipGetLastError();
     return e != hipSuccess ? e : join<float, D>(a, c, false, true, stream);

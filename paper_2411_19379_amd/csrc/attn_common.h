@@ -119,17 +119,23 @@ __device__ __forceinline__ Seq load_seq(const AttendArgs &a, int b)
     const int64_t from = a.cu[b] < 0 ? 0 : a.cu[b], to = a.cu[b + 1] > a.T ? a.T : a.cu[b + 1];
     s.start = (int)from;
     s.n = to > from ? (int)(to - from) : 0;
-    const int64_t most = (int64_t)a.max_blocks << a.log2_bs;  // tokens behind the table's end are not seen
-    const int64_t room = most > 0x3fffffff ? 0x3fffffff : most;
-    const int c = a.cached[b] < 0 ? 0 : a.cached[b];
-    s.cached = c > room ? (int)room : c;
+    const int c = a.cached[b];
+    s.cached = c < 0 ? 0 : c > 0x3fffffff ? 0x3fffffff : c;
     s.rows = s.n * a.group;
     return s;
 }
 
-// Keys that the rows [r0, r0 + ROWS) of a sequence see, in tiles of KT keys: first the sinks' tiles, then [near, end).
+// Keys behind the end of the table's rows do not exist.
+__device__ __forceinline__ int table_end(const AttendArgs &a)
+{
+    const int64_t keys = (int64_t)a.max_blocks << a.log2_bs;
+    return keys > 0x7fffffff ? 0x7fffffff : (int)keys;
+}
+
+// Keys that the rows [r0, r0 + ROWS) of a sequence see, in tiles of KT keys: first the sinks' tiles, then those from `near` on.
 struct KeyRange {
     int pos0, pos1;  // positions of the first and the last row
+    int end;         // no row sees this key or one behind it
     int near;        // first tile of the window
     int n_sink;      // tiles of sinks in front of it
     int n;           // tiles in all
@@ -141,17 +147,21 @@ template <int KT> __device__ __forceinline__ KeyRange key_range(const AttendArgs
     const int last = r0 + rows < s.rows ? r0 + rows - 1 : s.rows - 1;
     k.pos0 = s.cached + r0 / a.group;
     k.pos1 = s.cached + last / a.group;
+    const int most = table_end(a);
+    k.end = k.pos1 < most ? k.pos1 + 1 : most;
+    const int tiles = (k.end - 1) / KT + 1;
     const int lo = a.window > 0 && k.pos0 >= a.window ? k.pos0 - a.window + 1 : 0;
-    k.near = lo / KT;
+    k.near = lo / KT < tiles ? lo / KT : tiles;
     const int sink_tiles = a.sinks / KT + (a.sinks % KT != 0);
     k.n_sink = sink_tiles < k.near ? sink_tiles : k.near;
-    k.n = k.n_sink + k.pos1 / KT + 1 - k.near;
+    k.n = k.n_sink + tiles - k.near;
     return k;
 }
-// An upper bound of that over the sequence's row tiles.
+// How many steps the splits of a sequence are made for: those of its longest tile of rows, but for keys that the table has no
+// place for.  The host computes the same bound for any sequence (may_split).
 template <int KT> __device__ __forceinline__ int most_steps(const AttendArgs &a, const Seq &s, int rows)
 {
-    const int all = (s.cached + s.n - 1) / KT + 1;
+    const int most = table_end(a), all = ((s.cached + s.n < most ? s.cached + s.n : most) - 1) / KT + 1;
     if (a.window <= 0)
         return all;
     const int64_t near = ((int64_t)a.window + rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;

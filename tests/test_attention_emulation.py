@@ -142,6 +142,17 @@ def test_attend_with_blocks_missing(emu, tmp_path, name):
         assert np.all(out[0] == 0) and np.all(np.isneginf(lse[0]))
 
 
+@pytest.mark.parametrize("name", ["decode", "few_window", "chunk", "f32"])
+def test_attend_with_a_table_that_is_too_narrow(emu, tmp_path, name):
+    """Sequences longer than their rows of the table: the keys behind its end do not exist."""
+    p = ah.make(13, *CASES[name])
+    for width in (1, 3):
+        p.table = np.ascontiguousarray(ah.make(13, *CASES[name]).table[:, :width])
+        for target in (0, 40):
+            out, lse = _attend(emu, tmp_path, p, target=target)
+            ah.check(p, out, lse, f"{name} {width}")
+
+
 NOT_FINITE = ["few_window", "few_tokens", "chunk_window", "chunk_group", "f32_wide_window"]
 
 

@@ -36,6 +36,15 @@ def test_attend_with_blocks_missing(name):
     ah.check(p, *_attend(p), name)
 
 
+@pytest.mark.parametrize("name", ["decode", "few_window", "chunk", "f32"])
+def test_attend_with_a_table_that_is_too_narrow(name):
+    print(f"attend narrow table {name}", flush=True)
+    p = ah.make(13, *CASES[name])
+    for width in (1, 3):
+        p.table = np.ascontiguousarray(ah.make(13, *CASES[name]).table[:, :width])
+        ah.check(p, *_attend(p), f"{name} {width}")
+
+
 @pytest.mark.parametrize("where", ["v", "k"])
 @pytest.mark.parametrize("name", NOT_FINITE)
 def test_attend_not_finite(name, where):
