@@ -354,39 +354,54 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     memory_wait();
     if (!late)
         lds_barrier();
+    lds_barrier();  // the last tile has been read: LDS takes the results
     if (!wave_works)
         return;
     lsum += read_from(lsum, l ^ 32);
     const int seen_there = read_from((int)seen, l ^ 32);
-    seen = seen || seen_there != 0;
-    const float w = row_weight(lsum, m, seen);
-    if (!row_works)
+    const float w = row_weight(lsum, m, seen || seen_there != 0);
+    const bool split = it.n_splits > 1;
+    const int part = split ? part_of(a, it, kv_head, it.split) : 0;
+    if (split && part >= a.most_parts)
         return;
-    if (it.n_splits > 1) {
-        const int part = part_of(a, it, kv_head, it.split);
-        if (part >= a.most_parts)
-            return;
-        const int64_t at = (int64_t)part * a.rows_cap + row - r0;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<float4 *>(a.part + at * D + db * 32 + 8 * q + 4 * half) =
-                    make_float4(o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]);
-        if (half == 0)
-            *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(m, w);
-        return;
+    const int64_t part_row = (int64_t)part * a.rows_cap + 32 * wave;
+    if (row_works && half == 0) {
+        if (split)
+            *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + (part_row + l % 32) * 2) = make_float2(m, w);
+        else if (a.lse)
+            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
     }
-    const float scale = w == 0.f ? 0.f : w < 0.f ? NAN : 1.f / w;
-    uint16_t *const out = static_cast<uint16_t *>(a.out) + (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D;
+    // A lane holds values of one row all over the head: through LDS, half of the head at a time, to rows that leave in whole lines.
+    constexpr int COLS = D / 2, STRIDE = COLS + 4, LANES = COLS / 4, ROWS_AT_ONCE = 64 / LANES;
+    static_assert((size_t)NW * 32 * STRIDE * sizeof(float) <= 2 * kChunkBuffers * (size_t)Tile::kBytes, "fits");
+    const float scale = split ? 1.f : w == 0.f ? 0.f : w < 0.f ? NAN : 1.f / w;
+    float *const mine = reinterpret_cast<float *>(lds_raw) + wave * 32 * STRIDE;
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db)
+    for (int h = 0; h < 2; ++h) {
+        lds_wait();
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<uint2 *>(out + db * 32 + 8 * q + 4 * half) =
-                make_uint2(E::pack(o[db][4 * q] * scale, o[db][4 * q + 1] * scale), E::pack(o[db][4 * q + 2] * scale, o[db][4 * q + 3] * scale));
-    if (a.lse && half == 0)
-        a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
+        for (int db = 0; db < D / 64; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x16 &x = o[h * (D / 64) + db];
+                *reinterpret_cast<f32x4 *>(mine + l % 32 * STRIDE + db * 32 + 8 * q + 4 * half) =
+                    f32x4{x[4 * q] * scale, x[4 * q + 1] * scale, x[4 * q + 2] * scale, x[4 * q + 3] * scale};
+            }
+        lds_wait();
+#pragma unroll
+        for (int i = 0; i < 32 / ROWS_AT_ONCE; ++i) {
+            const int r = i * ROWS_AT_ONCE + l / LANES, d = h * COLS + l % LANES * 4;
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(mine + r * STRIDE + l % LANES * 4);
+            const int to_token = read_from(token, r), to_head = read_from(head, r);
+            if (r0 + 32 * wave + r >= s.rows)
+                continue;
+            if (split)
+                *reinterpret_cast<f32x4 *>(a.part + (part_row + r) * D + d) = x;
+            else
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + (int64_t)(s.start + to_token) * a.out_stride + (int64_t)to_head * D + d) =
+                    make_uint2(E::pack(x[0], x[1]), E::pack(x[2], x[3]));
+        }
+    }
 }
 
 // ================================================================ few rows
@@ -976,9 +991,10 @@ template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoi
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     for (int unit = blockIdx.x; unit < most_units; unit += workgroups) {
         Item it;
-        if (!find_item<ROWS, KT>(a, unit / blocks / a.Hkv, true, &it))
+        if (!find_item<ROWS, KT>(a, unit / a.Hkv / blocks, true, &it))
             return;
-        join_row<E, D, ROWS>(a, it, load_seq(a, it.seq), unit / blocks % a.Hkv, unit % blocks * kJoinRows + wave);
+        // key heads fastest, as in the kernels in front: a head's parts are read on the die that wrote them if 8 divide the heads
+        join_row<E, D, ROWS>(a, it, load_seq(a, it.seq), unit % a.Hkv, unit / a.Hkv % blocks * kJoinRows + wave);
     }
 }
 
