@@ -169,7 +169,8 @@ int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total
  *   scale   positive and finite
  *   max_new 0, or the largest number of new tokens of any sequence as far as
  *           the caller knows it: it decides between kernels for single tokens
- *           and for chunks and nothing else (a wrong value costs time)
+ *           and for chunks and nothing else (a wrong value costs time; 0 takes
+ *           a batch with no more tokens than sequences for single tokens)
  *   workspace  >= attn_workspace_bytes of the same batch, total_tokens and
  *           max_new; may be NULL if that is 0
  *

@@ -898,9 +898,8 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 // The rows of sequences whose keys were split, a wave per row: the lanes load the maxima and weights of up to 64 parts at once,
 // then the sums in the order of the parts, 64 * 4 / D parts per load and kJoinAhead loads on their way.
 constexpr int kJoinThreads = 256;
-constexpr int kJoinRows = kJoinThreads / 64;
 constexpr int kJoinAhead = 4;
-constexpr int kJoinWorkgroups = 1024;
+constexpr int kJoinWorkgroups = 2048;
 
 template <typename E> struct Out {
     static __device__ __forceinline__ void store4(void *out, int64_t at, const float *v)
@@ -984,17 +983,19 @@ template <typename E, int D, int ROWS> __device__ __forceinline__ void join_row(
         a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(j.m, j.weight(), a.scale_log2);
 }
 
-// kJoinRows rows at a time, `blocks` times per (tile, key head); the workgroups of the launch take them in turn until there are
+// `rows` rows at a time, `blocks` times per (tile, key head); the workgroups of the launch take them in turn until there are
 // no more.  (A workgroup for every piece that there might be took 48 us to find nothing to do for 32768 of them.)
-template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a, int blocks, int workgroups, int most_units)
+template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(AttendArgs a, int rows, int blocks, int workgroups, int most_units)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     for (int unit = blockIdx.x; unit < most_units; unit += workgroups) {
         Item it;
         if (!find_item<ROWS, KT>(a, unit / a.Hkv / blocks, true, &it))
             return;
+        const Seq s = load_seq(a, it.seq);
         // key heads fastest, as in the kernels in front: a head's parts are read on the die that wrote them if 8 divide the heads
-        join_row<E, D, ROWS>(a, it, load_seq(a, it.seq), unit % a.Hkv, unit / a.Hkv % blocks * kJoinRows + wave);
+        for (int r = wave; r < rows; r += kJoinThreads / 64)
+            join_row<E, D, ROWS>(a, it, s, unit % a.Hkv, unit / a.Hkv % blocks * rows + r);
     }
 }
 
@@ -1002,41 +1003,39 @@ template <typename E, int D, int ROWS, int KT> __global__ __launch_bounds__(kJoi
 constexpr int kChunkWaves = 8;
 constexpr int kChunkRows = 32 * kChunkWaves;
 constexpr int kF32Rows = 16 * kF32Waves;
+constexpr int kMostFewRows = 32;
 
-// One launch: which sequences, how many rows per tile, how many workgroups.
+// Rows per tile, workgroups, room for partial results.
 struct Launch {
     int rows;             // per tile
-    int64_t min_rows, max_rows;
     uint32_t target;
     int min_steps;
     int64_t most_tiles;   // of all sequences, per key head
-    int64_t grid, join_grid, join_units, join_blocks, parts, rows_cap;
+    int64_t grid, join_grid, join_units, join_rows, join_blocks, parts, rows_cap;
     size_t bytes;         // of workspace
 };
 struct Choice {
-    int n;
-    Launch launch[2];
-    bool chunk[2];
+    Launch launch;
+    bool chunk;
     int row_blocks;       // of the kernel for few rows
 };
 
-Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, int64_t min_rows, int64_t max_rows, uint32_t target, int min_steps)
+Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32_t target, int min_steps)
 {
     Launch c;
     const int64_t group = s.n_q_heads / s.n_kv_heads, all_rows = T * group, seqs = batch < T ? batch : T;
     c.rows = rows;
-    c.min_rows = min_rows;
-    c.max_rows = max_rows;
     c.target = ATTN_TARGET ? (uint32_t)(ATTN_TARGET) : target;
     c.min_steps = ATTN_TARGET ? 1 : min_steps;
-    c.most_tiles = max_rows <= rows ? seqs : all_rows / rows + seqs;
-    // A sequence of n steps per tile has ceil(n / per) <= n / per + 1 splits, and the sum of n / per over the tiles is at most
-    // the target.  Only sequences with n > per are split, whose ceil is at most 2 n / per.
+    c.most_tiles = all_rows / rows + seqs;
+    // A tile of a sequence of n steps has at most ceil(n / per) <= n / per + 1 splits, and the sum of n / per over the tiles is at
+    // most the target.  Only sequences with n > per are split, whose ceil is at most 2 n / per.
     c.grid = ((c.target + s.n_kv_heads - 1) / s.n_kv_heads + c.most_tiles) * s.n_kv_heads;
     c.parts = 2 * (int64_t)c.target;
     c.rows_cap = rows < all_rows ? rows : all_rows;
     const int64_t split_tiles = c.most_tiles * s.n_kv_heads < c.target ? c.most_tiles * s.n_kv_heads : c.target;
-    c.join_blocks = (c.rows_cap + kJoinRows - 1) / kJoinRows;
+    c.join_rows = c.rows_cap <= 16 ? 4 : 8;   // few rows: all at once; many: fewer look-ups of who they are
+    c.join_blocks = (c.rows_cap + c.join_rows - 1) / c.join_rows;
     c.join_units = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * c.join_blocks;
     c.join_grid = c.join_units < kJoinWorkgroups ? c.join_units : kJoinWorkgroups;
     // One sequence whose tiles alone are as many as the workgroups wanted has as many steps per workgroup as per tile: no split.
@@ -1046,29 +1045,24 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, int64_
     return c;
 }
 
+// One launch for the whole batch, by the most rows that a sequence may have: each kernel takes any.  (The kernel for chunks for
+// some sequences of a batch and the one for few rows for the others, a launch and a join each, lost nearly everywhere: 5
+// requests of 20 to 60 tokens 30.7 us against 25.9, 64 of 1 to 512 tokens 540 against 489, of 1 to 24 221 against 226.)  Without
+// a hint a batch with no more tokens than sequences is taken for single tokens.
 Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
 {
     Choice c;
-    const int64_t group = s.n_q_heads / s.n_kv_heads, most = max_new > 0 && max_new < T ? max_new : T, rows = most * group;
-    const int64_t any = (int64_t)1 << 40;
-    c.n = 1;
+    const int64_t group = s.n_q_heads / s.n_kv_heads, most = max_new > 0 ? (max_new < T ? max_new : T) : T <= batch ? 1 : T, rows = most * group;
     c.row_blocks = 1;
-    c.chunk[0] = true;
+    c.chunk = false;
     if (s.io_dtype == ATTN_DT_F32) {
-        c.launch[0] = make_launch(s, batch, T, kF32Rows, 0, any, 512, 16);
-        return c;
-    }
-    if (rows <= 64) {
-        c.chunk[0] = false;
-        c.row_blocks = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-        c.launch[0] = make_launch(s, batch, T, 16 * c.row_blocks, 0, any, 768, 4);
-        return c;
-    }
-    c.launch[0] = make_launch(s, batch, T, kChunkRows, batch > 1 ? 16 : 0, any, 512, 8);
-    if (batch > 1) {
-        c.n = 2;
-        c.chunk[1] = false;
-        c.launch[1] = make_launch(s, batch, T, 16, 0, 16, 768, 4);
+        c.launch = make_launch(s, batch, T, kF32Rows, 512, 16);
+    } else if (rows <= kMostFewRows) {
+        c.row_blocks = rows <= 16 ? 1 : 2;
+        c.launch = make_launch(s, batch, T, 16 * c.row_blocks, 768, 4);
+    } else {
+        c.chunk = true;
+        c.launch = make_launch(s, batch, T, kChunkRows, 256, 8);
     }
     return c;
 }
@@ -1090,15 +1084,13 @@ template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &
         return hipSuccess;
     const dim3 grid((unsigned)c.join_grid), block(kJoinThreads);
     if (f32)
-        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<float, D, kF32Rows, kF32Keys>), grid, block, 0, stream, a, (int)c.join_rows, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (!few)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, kChunkRows, kChunkKeys>), grid, block, 0, stream, a, (int)c.join_rows, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else if (c.rows == 16)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
-    else if (c.rows == 32)
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 16, kFewKeys>), grid, block, 0, stream, a, (int)c.join_rows, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     else
-        hipLaunchKernelGGL((attn_join_kernel<E, D, 64, kFewKeys>), grid, block, 0, stream, a, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
+        hipLaunchKernelGGL((attn_join_kernel<E, D, 32, kFewKeys>), grid, block, 0, stream, a, (int)c.join_rows, (int)c.join_blocks, (int)c.join_grid, (int)c.join_units);
     return hipGetLastError();
 }
 
@@ -1131,7 +1123,7 @@ template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Laun
             hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves, false>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
         e = hipGetLastError();
     } else {
-        e = c.rows == 16 ? launch_few<E, D, 1>(a, c, stream) : c.rows == 32 ? launch_few<E, D, 2>(a, c, stream) : launch_few<E, D, 4>(a, c, stream);
+        e = c.rows == 16 ? launch_few<E, D, 1>(a, c, stream) : launch_few<E, D, 2>(a, c, stream);
     }
     return e != hipSuccess ? e : join<E, D>(a, c, !chunk, false, stream);
 }
@@ -1153,11 +1145,7 @@ size_t attn_attend_workspace(const attn_shape_t &s, int batch, int64_t T, int ma
 {
     if (T == 0 || batch == 0)
         return 0;
-    const Choice c = choose(s, batch, T, max_new);
-    size_t n = 0;
-    for (int i = 0; i < c.n; ++i)
-        n += (c.launch[i].bytes + 255) / 256 * 256;
-    return n;
+    return choose(s, batch, T, max_new).launch.bytes;
 }
 
 hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
@@ -1166,9 +1154,9 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
                               void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream)
 {
     const Choice c = choose(s, batch, T, max_new);
-    for (int i = 0; i < c.n; ++i)
-        if (c.launch[i].grid > 0x7fffffff || c.launch[i].join_units > 0x7fffffff - kJoinWorkgroups)
-            return hipErrorInvalidValue;
+    const Launch &u = c.launch;
+    if (u.grid > 0x7fffffff || u.join_units > 0x7fffffff - kJoinWorkgroups)
+        return hipErrorInvalidValue;
     AttendArgs a;
     a.q = q;
     a.k_cache = k_cache;
@@ -1192,26 +1180,14 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.window = window < kMostWindow ? window : kMostWindow;
     a.sinks = sinks;
     a.scale_log2 = scale * kLog2e;
-    unsigned char *ws = static_cast<unsigned char *>(workspace);
-    for (int i = 0; i < c.n; ++i) {
-        const Launch &u = c.launch[i];
-        a.part = reinterpret_cast<float *>(ws);
-        ws += (u.bytes + 255) / 256 * 256;
-        a.min_rows = (int)u.min_rows;
-        a.max_rows = u.max_rows > 0x7fffffff ? 0x7fffffff : (int)u.max_rows;
-        a.rows_cap = (int)u.rows_cap;
-        a.most_parts = (int)u.parts;
-        a.target = u.target;
-        a.min_steps = u.min_steps;
-        hipError_t e;
-        if (s.io_dtype == ATTN_DT_F32)
-            e = s.head_dim == 64 ? launch_f32<64>(a, u, stream) : launch_f32<128>(a, u, stream);
-        else if (s.io_dtype == ATTN_DT_BF16)
-            e = s.head_dim == 64 ? launch16<Bf16, 64>(a, u, c.chunk[i], stream) : launch16<Bf16, 128>(a, u, c.chunk[i], stream);
-        else
-            e = s.head_dim == 64 ? launch16<F16, 64>(a, u, c.chunk[i], stream) : launch16<F16, 128>(a, u, c.chunk[i], stream);
-        if (e != hipSuccess)
-            return e;
-    }
-    return hipSuccess;
+    a.part = static_cast<float *>(workspace);
+    a.rows_cap = (int)u.rows_cap;
+    a.most_parts = (int)u.parts;
+    a.target = u.target;
+    a.min_steps = u.min_steps;
+    if (s.io_dtype == ATTN_DT_F32)
+        return s.head_dim == 64 ? launch_f32<64>(a, u, stream) : launch_f32<128>(a, u, stream);
+    if (s.io_dtype == ATTN_DT_BF16)
+        return s.head_dim == 64 ? launch16<Bf16, 64>(a, u, c.chunk, stream) : launch16<Bf16, 128>(a, u, c.chunk, stream);
+    return s.head_dim == 64 ? launch16<F16, 64>(a, u, c.chunk, stream) : launch16<F16, 128>(a, u, c.chunk, stream);
 }

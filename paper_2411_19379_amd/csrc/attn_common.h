@@ -99,7 +99,6 @@ struct AttendArgs {
     int32_t log2_bs, max_blocks, n_blocks;
     int32_t window, sinks;
     float scale_log2;       // scale * log2(e): the softmax runs on powers of two
-    int32_t min_rows, max_rows;  // this launch takes the sequences with min_rows < rows <= max_rows
     int32_t rows_cap;       // rows of a partial result
     int32_t most_parts;     // partial results there is room for
     uint32_t target;        // workgroups that keep the GPU busy
@@ -200,13 +199,22 @@ struct SeenTiles {
 };
 
 // ---------------------------------------------------------------- who does what
-// The rows of a sequence are cut into tiles of ROWS rows; the keys of all tiles of a sequence into the same number of
-// splits, as many as it takes to give the GPU `target` workgroups of equal length.  Every workgroup finds its own piece
-// from the lengths: nothing is planned ahead, so the lengths may change between replays of a graph.
+// The rows of a sequence are cut into tiles of ROWS rows.  With `per` the steps of a workgroup if the GPU's `target` workgroups
+// shared all steps, the tiles at a sequence's front that take no more than `per` stay whole, and the keys of all others are cut
+// into the same number of splits.  Every
+// workgroup finds its own piece from the lengths: nothing is planned ahead, so the lengths may change between replays of a graph.
 struct Item {
     int seq, tile, split, n_splits;
-    int part;  // the first partial result of (seq, tile): split s of key head h is part + (tile * n_splits + s) * Hkv + h
+    int part;  // partial result: split s of key head h of this tile is (part + s) * Hkv + h
 };
+// How many of a sequence's first tiles take no more than `per` steps.  (With a window the steps hardly depend on the tile.)
+template <int ROWS, int KT> __device__ __forceinline__ int whole_tiles(const AttendArgs &a, const Seq &s, int tiles, uint32_t per)
+{
+    if (a.window > 0)
+        return 0;
+    const int64_t rows = ((int64_t)per * KT - s.cached) * a.group;  // those that see no key behind per * KT
+    return rows <= 0 ? 0 : rows >= s.rows ? tiles : (int)(rows / ROWS);
+}
 
 // The `unit`-th (tile, split) of the launch, or with `of_join` the unit-th tile of the sequences that are split; false if there is
 // none.  Every wave finds out for itself, PER sequences per lane at a time: no barrier, one trip to memory for up to 64 PER
@@ -215,15 +223,15 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
 {
     constexpr int ALL = 64 * PER;
     const int l = lane_id();
+    Seq seq[PER];
     int tiles[PER], steps[PER];
     auto load = [&](int b0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             const int b = b0 + l * PER + u;
-            const Seq s = load_seq(a, b < a.batch ? b : a.batch - 1);
-            const bool mine = b < a.batch && s.rows > a.min_rows && s.rows <= a.max_rows;
-            tiles[u] = mine ? (s.rows + ROWS - 1) / ROWS : 0;
-            steps[u] = mine ? most_steps<KT>(a, s, ROWS) : 0;
+            seq[u] = load_seq(a, b < a.batch ? b : a.batch - 1);
+            tiles[u] = b < a.batch ? (seq[u].rows + ROWS - 1) / ROWS : 0;
+            steps[u] = tiles[u] > 0 ? most_steps<KT>(a, seq[u], ROWS) : 0;
         }
     };
     uint32_t work = 0;  // steps of all workgroups
@@ -244,39 +252,48 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
     for (int b0 = 0; b0 < a.batch; b0 += ALL) {
         if (a.batch > ALL)
             load(b0);
-        int splits[PER], items = 0, parts = 0;
+        int splits[PER], whole[PER], items = 0, parts = 0;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             splits[u] = (int)(((uint32_t)steps[u] + per - 1) / per);
-            items += tiles[u] * (of_join ? splits[u] > 1 : splits[u]);
-            parts += splits[u] > 1 ? tiles[u] * splits[u] : 0;
+            whole[u] = splits[u] > 1 ? whole_tiles<ROWS, KT>(a, seq[u], tiles[u], per) : tiles[u];
+            const int cut = tiles[u] - whole[u];
+            items += of_join ? cut : whole[u] + cut * splits[u];
+            parts += cut * splits[u];
         }
         const int items_upto = wave_scan(items), parts_upto = wave_scan(parts);
         int at = unit - items_before - (items_upto - items);
         const uint64_t here = __ballot(at >= 0 && at < items);
         if (here != 0) {
-            int seq = 0, n_splits = 1, in_seq = 0, of_seq = 1, part = parts_before + parts_upto - parts;
-            bool found = false;
+            int found = 0, n_splits = 1, n_whole = 0, left = 0, part = parts_before + parts_upto - parts;
+            bool done = false;
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
-                const int n = tiles[u] * (of_join ? splits[u] > 1 : splits[u]);
-                if (!found && at < n) {
-                    seq = b0 + l * PER + u, n_splits = splits[u], in_seq = at, of_seq = n;
-                    found = true;
+                const int cut = tiles[u] - whole[u], n = of_join ? cut : whole[u] + cut * splits[u];
+                if (!done && at < n) {
+                    found = b0 + l * PER + u, n_splits = splits[u], n_whole = whole[u], left = n - 1 - at;  // the last rows, which see the most keys, first
+                    done = true;
                 }
-                if (!found) {
+                if (!done) {
                     at -= n;
-                    part += splits[u] > 1 ? tiles[u] * splits[u] : 0;
+                    part += cut * splits[u];
                 }
             }
             const int owner = __builtin_ctzll(here);
-            out->seq = __builtin_amdgcn_readlane(seq, owner);
-            out->n_splits = __builtin_amdgcn_readlane(n_splits, owner);
-            out->part = __builtin_amdgcn_readlane(part, owner);
-            // the last rows, which see the most keys, first
-            const int left = __builtin_amdgcn_readlane(of_seq, owner) - 1 - __builtin_amdgcn_readlane(in_seq, owner), per_tile = of_join ? 1 : out->n_splits;
-            out->tile = left / per_tile;
-            out->split = left - out->tile * per_tile;
+            out->seq = __builtin_amdgcn_readlane(found, owner);
+            n_splits = __builtin_amdgcn_readlane(n_splits, owner);
+            n_whole = __builtin_amdgcn_readlane(n_whole, owner);
+            left = __builtin_amdgcn_readlane(left, owner);
+            part = __builtin_amdgcn_readlane(part, owner);
+            if (!of_join && left < n_whole) {
+                out->tile = left, out->split = 0, out->n_splits = 1, out->part = 0;
+                return true;
+            }
+            const int of_cut = of_join ? left * n_splits : left - n_whole, tile = of_cut / n_splits;
+            out->tile = n_whole + tile;
+            out->split = of_cut - tile * n_splits;
+            out->n_splits = n_splits;
+            out->part = part + tile * n_splits;
             return true;
         }
         items_before += __builtin_amdgcn_readlane(items_upto, 63);
@@ -290,7 +307,7 @@ template <int ROWS, int KT> __device__ __forceinline__ bool find_item(const Atte
 }
 __device__ __forceinline__ int part_of(const AttendArgs &a, const Item &it, int kv_head, int split)
 {
-    return (it.part + it.tile * it.n_splits + split) * a.Hkv + kv_head;
+    return (it.part + split) * a.Hkv + kv_head;
 }
 
 // ---------------------------------------------------------------- the cache
