@@ -418,7 +418,7 @@ template <int D> struct FewTile {
     static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4); }
 };
 
-template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
+template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
 {
     typedef FewTile<D> Tile;
     constexpr int ROWS = 16 * RB, PIECES = Tile::kPieces;
@@ -467,30 +467,65 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
         for (int db = 0; db < D / 16; ++db)
             o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    // With WIDE, blocks of at least 16 keys, a tile's keys lie in two blocks: scalar look-ups, and every load is a uniform address
+    // and an offset that does not change (32 sequences of one token, 32 rows of heads: 114 us, with a look-up per lane 126).  A key that does not exist is read from the cache's first rows: as K it comes to nothing
+    // in the softmax, as V it is cleared.
+    const int32_t *const table = a.table + (int64_t)it.seq * a.max_blocks;
+    const int bs_mask = (1 << a.log2_bs) - 1;
+    const uint32_t k_offset = l % 16 * D * 2 + 16 * quarter, v_offset = l * 16;
+    constexpr int V_HALF = V_LOADS / 2;  // loads of 16 rows of V
     uint4 kreg[2][KS], vreg[V_LOADS];
-    int block = -1, row_of_key = -1;  // of key l % 32 of a tile: of the one behind the next, of the next
-    uint64_t exist_next = 0;
-    auto look_up = [&](int step) __attribute__((always_inline)) { block = step < step_end ? table_entry(a, it.seq, keys.tile(step) * kFewKeys + l % 32, end) : -1; };
+    int block[2] = {-1, -1};    // of the tile behind the next: WIDE of its halves, else [0] of key l % 32
+    uint32_t exist_next = 0;
+    int row_of_key = -1;
+    auto look_up = [&](int step) __attribute__((always_inline)) {
+        const int j0 = keys.tile(step) * kFewKeys;
+        if (WIDE) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = (j0 + 16 * h) >> a.log2_bs;
+                block[h] = scalar_load(table + ((uint32_t)e < (uint32_t)a.max_blocks ? e : a.max_blocks - 1));
+            }
+        } else {
+            const int e = (j0 + l % 32) >> a.log2_bs;
+            block[0] = table[(uint32_t)e < (uint32_t)a.max_blocks ? e : a.max_blocks - 1];
+        }
+    };
     auto request = [&](int step) __attribute__((always_inline)) {
-        row_of_key = cache_row(a, block, kv_head, keys.tile(step) * kFewKeys + l % 32);
-        exist_next = __ballot(row_of_key >= 0);
-        const uint16_t *const k = static_cast<const uint16_t *>(a.k_cache), *const v = static_cast<const uint16_t *>(a.v_cache);
+        const int j0 = keys.tile(step) * kFewKeys;
+        if (WIDE) {
+            exist_next = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = j0 + 16 * h;
+                const bool there = j < end && (uint32_t)block[h] < (uint32_t)a.n_blocks;
+                const uint32_t row = there ? (uint32_t)(((block[h] * a.Hkv + kv_head) << a.log2_bs) + (j & bs_mask)) : 0u;
+                exist_next |= there ? 0xffffu << (16 * h) : 0u;
+                const unsigned char *const k = static_cast<const unsigned char *>(a.k_cache) + (uint64_t)row * (D * 2);
+                const unsigned char *const v = static_cast<const unsigned char *>(a.v_cache) + (uint64_t)row * (D * 2);
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks)
+                    kreg[h][ks] = *reinterpret_cast<const uint4 *>(k + k_offset + ks * 64);
+#pragma unroll
+                for (int i = 0; i < V_HALF; ++i)
+                    vreg[h * V_HALF + i] = *reinterpret_cast<const uint4 *>(v + v_offset + i * 1024);
+            }
+            return;
+        }
+        const int j = j0 + l % 32;
+        row_of_key = j < end && (uint32_t)block[0] < (uint32_t)a.n_blocks ? ((block[0] * a.Hkv + kv_head) << a.log2_bs) + (j & bs_mask) : -1;
+        exist_next = (uint32_t)__ballot(row_of_key >= 0);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const int r = read_from(row_of_key, 16 * kb + l % 16);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                kreg[kb][ks] = make_uint4(0, 0, 0, 0);
-                if (r >= 0)
-                    kreg[kb][ks] = *reinterpret_cast<const uint4 *>(k + (int64_t)r * D + ks * 32 + 8 * quarter);
-            }
+            for (int ks = 0; ks < KS; ++ks)
+                kreg[kb][ks] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.k_cache) + (int64_t)(r < 0 ? 0 : r) * D + ks * 32 + 8 * quarter);
         }
 #pragma unroll
         for (int i = 0; i < V_LOADS; ++i) {
             const int r = read_from(row_of_key, i * V_ROWS + l / PIECES);
-            vreg[i] = make_uint4(0, 0, 0, 0);
-            if (r >= 0)
-                vreg[i] = *reinterpret_cast<const uint4 *>(v + (int64_t)r * D + l % PIECES * 8);
+            vreg[i] = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.v_cache) + (int64_t)(r < 0 ? 0 : r) * D + l % PIECES * 8);
         }
     };
     if (step_begin + wave < step_end) {
@@ -502,7 +537,7 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
     for (int step = step_begin + wave; step < step_end; step += kFewWaves) {
         const int j0 = keys.tile(step) * kFewKeys;
         const bool part_seen = !seen_tiles.all(j0);
-        const uint32_t exist = (uint32_t)exist_next;
+        const uint32_t exist = exist_next;
         f32x4 st[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
@@ -514,6 +549,15 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
                     st[rb][kb] = E::mfma16(kreg[kb][ks], qf[rb][ks], st[rb][kb]);
             }
         uint32_t bad = 0;  // keys whose V is not finite
+        if (exist != 0xffffffffu || j0 + kFewKeys > end) {
+            const int l2 = unknown(l);
+#pragma unroll
+            for (int i = 0; i < V_LOADS; ++i) {
+                const int r = i * V_ROWS + l2 / PIECES;
+                const bool there = (exist >> r & 1) != 0 && j0 + r < end;
+                vreg[i] = make_uint4(there ? vreg[i].x : 0u, there ? vreg[i].y : 0u, there ? vreg[i].z : 0u, there ? vreg[i].w : 0u);
+            }
+        }
         if (part_seen) {
 #pragma unroll
             for (int i = 0; i < V_LOADS; ++i) {
@@ -590,7 +634,7 @@ template <typename E, int D, int RB> __global__ __launch_bounds__(64 * kFewWaves
         }
         for (uint32_t left = bad; left != 0; left &= left - 1) {
             const int key = __builtin_ctz(left), e_of = 4 * (key / 16) + key % 4, from = key % 16 / 4;
-            const int cr = cache_row(a, table_entry(a, it.seq, j0 + key, end), kv_head, j0 + key);
+            const int e = (j0 + key) >> a.log2_bs, cr = cache_row(a, j0 + key < end && e < a.max_blocks ? table[e] : -1, kv_head, j0 + key);
             const uint16_t *v_row = static_cast<const uint16_t *>(a.v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
@@ -1104,7 +1148,10 @@ template <typename E, int D, int RB> hipError_t launch_few(const AttendArgs &a, 
 {
     constexpr size_t v = (size_t)kFewWaves * FewTile<D>::kBytes, o = (size_t)kFewWaves * 16 * (D + 4 + 2) * sizeof(float);
     constexpr size_t lds = v > o ? v : o;
-    hipLaunchKernelGGL((attn_few_kernel<E, D, RB>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
+    if (1 << a.log2_bs >= 16)
+        hipLaunchKernelGGL((attn_few_kernel<E, D, RB, true>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
+    else
+        hipLaunchKernelGGL((attn_few_kernel<E, D, RB, false>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
     return hipGetLastError();
 }
 

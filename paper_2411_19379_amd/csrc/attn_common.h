@@ -319,11 +319,6 @@ __device__ __forceinline__ int cache_row(const AttendArgs &a, int block, int kv_
         return -1;
     return ((block * a.Hkv + kv_head) << a.log2_bs) + (j & ((1 << a.log2_bs) - 1));
 }
-__device__ __forceinline__ int table_entry(const AttendArgs &a, int seq, int j, int end)
-{
-    const int e = j >> a.log2_bs;
-    return j < end && e < a.max_blocks ? a.table[(int64_t)seq * a.max_blocks + e] : -1;
-}
 
 // ---------------------------------------------------------------- 16-bit types
 struct Bf16 {
