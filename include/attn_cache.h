@@ -24,7 +24,10 @@
  * Sequence b of a packed batch has cached_lens[b] tokens in the cache and
  * brings n_b = cu_seqlens[b+1] - cu_seqlens[b] new ones; token i of them has
  * position cached_lens[b] + i.  Its key at position j lies in block
- * table[b, j / block_size], row j % block_size.  The caches of a layer are
+ * table[b, j / block_size], row j % block_size.  cu_seqlens[batch] may be less
+ * than total_tokens (a captured step with room for more): the tokens behind it
+ * belong to no sequence, get the slot -1 and position 0, and their rows of the
+ * attention's results are not written.  The caches of a layer are
  *
  *   k_cache, v_cache  [n_blocks, n_kv_heads, block_size, head_dim]  io_dtype
  *
@@ -72,7 +75,7 @@ typedef struct {
  * extends them.  Requests are served in order; the k-th block handed out is
  * free_blocks[n_free - 1 - k].
  *
- *   cu_seqlens   [batch+1]  int32 device; total_tokens = cu_seqlens[batch]
+ *   cu_seqlens   [batch+1]  int32 device, from 0 to at most total_tokens
  *   cached_lens  [batch]    int32 device
  *   shared_tail  [batch]    int32 device or NULL; nonzero: the sequence's last
  *                           cached block may be read by others (the hit ends

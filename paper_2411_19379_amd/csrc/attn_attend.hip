@@ -1082,9 +1082,6 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32
     c.join_blocks = (c.rows_cap + c.join_rows - 1) / c.join_rows;
     c.join_units = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * c.join_blocks;
     c.join_grid = c.join_units < kJoinWorkgroups ? c.join_units : kJoinWorkgroups;
-    // One sequence whose tiles alone are as many as the workgroups wanted has as many steps per workgroup as per tile: no split.
-    if (batch == 1 && (all_rows + rows - 1) / rows * s.n_kv_heads >= c.target)
-        c.join_grid = c.parts = 0;
     c.bytes = (size_t)(c.parts * c.rows_cap) * (s.head_dim + 2) * sizeof(float);
     return c;
 }
@@ -1220,7 +1217,6 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.Hq = s.n_q_heads;
     a.Hkv = s.n_kv_heads;
     a.group = s.n_q_heads / s.n_kv_heads;
-    a.D = s.head_dim;
     a.log2_bs = __builtin_ctz((unsigned)s.block_size);
     a.max_blocks = max_blocks;
     a.n_blocks = n_blocks;

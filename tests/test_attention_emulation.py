@@ -206,6 +206,77 @@ def test_attend_large_scores(emu, tmp_path):
             ah.check(p, out, lse, dtype, sums=0.0 if dtype != "f32" else 40.0 * 0.5 * 200 * p.scale)
 
 
+# More sequences than a wave looks up at once, and than it looks up four to a lane.
+MANY = {
+    "few_70": (2, 1, 64, 16, "bf16", [1] * 70, [(37 * i) % 150 for i in range(70)], 0, 0, 1),
+    "few_300": (1, 1, 64, 8, "f16", [i % 7 != 3 for i in range(300)], [(5 * i) % 41 for i in range(299)] + [170], 0, 0, 1),
+    "few_300_window": (2, 2, 64, 8, "f16", [i % 3 for i in range(300)], [(5 * i) % 41 for i in range(299)] + [170], 9, 2, 2),
+    "chunk_70": (2, 1, 64, 16, "bf16", [i % 4 for i in range(68)] + [70, 3], [(11 * i) % 60 for i in range(69)] + [300], 0, 0, 0),
+    "chunk_300": (1, 1, 64, 16, "f16", [40] + [i % 2 for i in range(298)] + [60], [0] + [i % 19 for i in range(298)] + [130], 0, 0, 60),
+    "f32_300": (1, 1, 64, 16, "f32", [i % 2 for i in range(299)] + [40], [i % 19 for i in range(299)] + [70], 0, 0, 0),
+}
+
+
+def many(name):
+    hq, hkv, d, bs, dtype, new, *rest = MANY[name]
+    return ah.make(17, hq, hkv, d, bs, dtype, [int(n) for n in new], *rest)
+
+
+@pytest.mark.parametrize("target", [0, 900])
+@pytest.mark.parametrize("name", sorted(MANY))
+def test_attend_many_sequences(emu, tmp_path, name, target):
+    p = many(name)
+    ah.check(p, *_attend(emu, tmp_path, p, target=target), name)
+
+
+# heads, key heads, head_dim, block size, type, new tokens (the last ones belong to no sequence), cached tokens
+PADDED = {
+    "chunk": (2, 1, 64, 16, "bf16", [10, 600], [300, 0], 0, 0, 0),
+    "chunk_three": (2, 1, 64, 16, "f16", [70, 0, 3, 200], [300, 5, 40, 0], 0, 0, 0),
+    "few": (4, 2, 128, 16, "bf16", [1, 1, 30], [260, 40, 0], 0, 0, 1),
+    "f32": (2, 1, 64, 16, "f32", [3, 130], [150, 0], 0, 0, 0),
+    "nothing": (2, 1, 64, 16, "bf16", [0, 90], [150, 0], 0, 0, 0),
+}
+
+
+class Padded(ah.Problem):
+    """A problem with more rows than its sequences have tokens."""
+
+    @property
+    def T(self):
+        return int(self.q.shape[0])
+
+
+def padded(name):
+    p = ah.make(19, *PADDED[name])
+    return Padded(**dict(vars(p), new=p.new[:-1], cached=p.cached[:-1], table=np.ascontiguousarray(p.table[:-1]), cu=p.cu[:-1]))
+
+
+def check_padded(p, out, lse, what):
+    n = int(p.cu[-1])
+    ah.check(p, out[:n], lse[:n], what, ref=[x[:n] for x in ah.reference(p)])
+
+
+@pytest.mark.parametrize("target", [0, 2, 30])
+@pytest.mark.parametrize("name", sorted(PADDED))
+def test_attend_rows_of_no_sequence(emu, tmp_path, name, target):
+    """cu_seqlens ends in front of the rows' end, as in a captured step with room for more tokens; a single sequence that has few
+    of them and many keys is split all the same."""
+    p = padded(name)
+    check_padded(p, *_attend(emu, tmp_path, p, target=target), name)
+
+
+@pytest.mark.parametrize("name", ["chunk", "few"])
+def test_attend_widest_window(emu, tmp_path, name):
+    """Windows and sinks up to the type's largest see what no window sees."""
+    p = ah.make(11, *CASES["chunk_group" if name == "chunk" else "few_tokens"])
+    ref = ah.reference(p)
+    for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1)):
+        p.window, p.sinks = window, sinks
+        for target in (0, 40):
+            ah.check(p, *_attend(emu, tmp_path, p, target=target), f"{name} {window} {sinks}", ref=ref)
+
+
 ASSIGN = {
     "one": (16, [137], [1001], True, 64),
     "mixed": (8, [1, 0, 30, 8, 5, 0, 17], [0, 12, 7, 8, 9, 8, 1], True, 40),

@@ -128,3 +128,19 @@ def test_rotary_table():
                dict(max_positions=4, rotary_dim=32, slow_turns=9.0, fast_turns=9.0)):
         with pytest.raises(ValueError):
             attn.rotary_table(device="cpu", **kw)
+
+
+def test_entry_points_refuse_host_tensors():
+    """There is no path without a GPU: tensors elsewhere are refused by name, and things that are no tensors by type."""
+    if not os.path.exists(b.ATTN_BINDING_PATH):
+        b.build_attention_binding()
+    ints = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises((ValueError, RuntimeError)):
+        attn.assign_blocks(16, 1, ints, ints[:1], ints.view(1, 2), ints, ints[:1])
+    x, cache = torch.zeros(1, 2, 64), torch.zeros(2, 2, 16, 64)
+    with pytest.raises((ValueError, RuntimeError)):
+        attn.rope_append(x, x, x, ints[:1], ints[:1].long(), None, cache, cache)
+    with pytest.raises((ValueError, RuntimeError)):
+        attn.attend(x, cache, cache, ints.view(1, 2), ints, ints[:1])
+    with pytest.raises(TypeError):
+        attn.attend(x, cache, cache, None, ints, ints[:1])

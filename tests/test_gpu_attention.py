@@ -5,7 +5,7 @@ import torch
 
 import attn_helpers as ah
 import attn_oracle
-from test_attention_emulation import ASSIGN, CASES, NOT_FINITE, ROPE, rope_check, rope_problem
+from test_attention_emulation import ASSIGN, CASES, MANY, NOT_FINITE, PADDED, ROPE, check_padded, many, padded, rope_check, rope_problem
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -155,6 +155,105 @@ def test_attend_offsets_beyond_32_bits():
         out, lse = attn.attend(p.q.to(DEV), k, v, _dev(table), _dev(p.cu), _dev(np.array(cached, np.int32)), scale=p.scale,
                                max_new=max_new, return_lse=True)
         ah.check(p, out.double().cpu().numpy(), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("name", sorted(MANY))
+def test_attend_many_sequences(name):
+    print(f"attend many {name}", flush=True)
+    p = many(name)
+    ah.check(p, *_attend(p), name)
+
+
+@pytest.mark.parametrize("name", sorted(PADDED))
+def test_attend_rows_of_no_sequence(name):
+    print(f"attend padded {name}", flush=True)
+    p = padded(name)
+    check_padded(p, *_attend(p), name)
+
+
+def test_attend_a_long_sequence_in_a_step_with_room_for_a_prompt():
+    """One token over many keys where the call has rows for a prompt: it is split, and the other rows of `out` stay."""
+    from paper_2411_19379_amd import attention as attn
+    p = ah.make(8, 8, 2, 128, 16, "bf16", [1], [9000])
+    q = torch.zeros((40000, p.hq, p.d), dtype=p.q.dtype, device=DEV)
+    q[:1] = p.q.to(DEV)
+    out = torch.full_like(q, 7.0)
+    _, lse = attn.attend(q, p.k_cache.to(DEV), p.v_cache.to(DEV), _dev(p.table), _dev(p.cu), _dev(np.array(p.cached, np.int32)),
+                         scale=p.scale, out=out, return_lse=True)
+    ah.check(p, out[:1].double().cpu().numpy(), lse[:1].cpu().numpy(), ref=_reference64(p))
+    assert bool((out[1:] == 7.0).all())
+
+
+def test_attend_widest_window():
+    p = ah.make(11, *CASES["chunk_group"])
+    ref = ah.reference(p)
+    for p.window, p.sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1)):
+        ah.check(p, *_attend(p), f"{p.window} {p.sinks}", ref=ref)
+
+
+@pytest.mark.parametrize("name", ["decode", "decode_group16", "few_tokens", "few_tokens_wide"])
+def test_attend_without_the_hint(name):
+    """The number of new tokens picks a kernel and nothing else."""
+    p = ah.make(11, *CASES[name])
+    ref = ah.reference(p)
+    for p.max_new in (0, 1, 3, 10 ** 6):
+        ah.check(p, *_attend(p), f"{name} {p.max_new}", ref=ref)
+
+
+def test_nothing_to_do():
+    """No sequences, no tokens: empty results, nothing touched."""
+    from paper_2411_19379_amd import attention as attn
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)
+    k = torch.ones((4, 2, 16, 64), dtype=torch.bfloat16, device=DEV)
+    q, kv = torch.empty((0, 4, 64), dtype=k.dtype, device=DEV), torch.empty((0, 2, 64), dtype=k.dtype, device=DEV)
+    for batch in (0, 3):
+        s = attn.assign_blocks(16, 0, ints(batch + 1), ints(batch), ints(batch, 5) - 1, ints(8), ints(1) + 8)
+        assert s.slots.numel() == 0 and s.positions.numel() == 0 and s.table.shape == (batch, 5) and bool((s.copies[:, :2] == -1).all())
+        if batch:
+            assert s.counts.tolist() == [8, 0]
+        assert attn.rope_append(q, kv, kv, s.positions, s.slots, attn.rotary_table(8, 64), k, k.clone(), copies=s.copies).shape == q.shape
+        out, lse = attn.attend(q, k, k, s.table, ints(batch + 1), ints(batch), return_lse=True)
+        assert out.shape == q.shape and lse.shape == (0, 4)
+    assert bool((k == 1).all())
+
+
+def _refused():
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device=DEV)
+    h = lambda *s: z(*s, t=torch.bfloat16)
+    assign = dict(block_size=16, total_tokens=3, cu_seqlens=z(3), cached_lens=z(2), table=z(2, 4), free_blocks=z(8), n_free=z(1))
+    rope = dict(q=h(3, 4, 64), k=h(3, 2, 64), v=h(3, 2, 64), positions=z(3), slots=z(3, t=torch.int64) - 1, rotary=z(9, 2, 32, t=torch.float32),
+                k_cache=h(5, 2, 16, 64), v_cache=h(5, 2, 16, 64))
+    attend = dict(q=h(3, 4, 64), k_cache=h(5, 2, 16, 64), v_cache=h(5, 2, 16, 64), table=z(2, 4), cu_seqlens=z(3), cached_lens=z(2))
+    wide = h(3, 2, 4, 64)
+    return [
+        ("assign_blocks", assign, [
+            (dict(cu_seqlens=z(3, t=torch.int64)), ValueError), (dict(cached_lens=z(3)), ValueError), (dict(table=z(4, 4)[::2]), ValueError),
+            (dict(n_free=z(2)), ValueError), (dict(shared_tail=z(3)), ValueError), (dict(total_tokens=-1), ValueError),
+            (dict(free_blocks=torch.zeros(8, dtype=torch.int32)), ValueError), (dict(block_size=24), RuntimeError), (dict(table=None), TypeError),
+            (dict(block_size="16"), TypeError), (dict(block_size=2 ** 40), ValueError), (dict(cu_seqlens=torch.zeros(3, dtype=torch.int32)), ValueError)]),
+        ("rope_append", rope, [
+            (dict(q=h(3, 4, 64).float()), ValueError), (dict(q=h(4, 4, 64)), ValueError), (dict(k=h(3, 4, 64)), ValueError), (dict(q=wide[:, 0, :, ::2]), ValueError),
+            (dict(q=h(3, 64, 4).transpose(1, 2)), ValueError), (dict(slots=z(3)), ValueError),
+            (dict(rotary=z(9, 2, 32)), ValueError), (dict(positions=None), TypeError), (dict(k_cache=h(5, 2, 64)), ValueError),
+            (dict(v_cache=h(5, 2, 16, 32)), ValueError), (dict(rotary=z(9, 2, 64, t=torch.float32)), RuntimeError), (dict(copies=z(2, 3)), ValueError),
+            (dict(q_out=h(3, 4, 32)), ValueError), (dict(q=h(3, 3, 64)), RuntimeError)]),
+        ("attend", attend, [
+            (dict(q=h(3, 4, 32)), ValueError), (dict(q=h(12, 64)), ValueError), (dict(cu_seqlens=z(4)), ValueError), (dict(table=z(2, 4).long()), ValueError),
+            (dict(scale=0.0), RuntimeError), (dict(scale=float("nan")), RuntimeError), (dict(window=-1), RuntimeError), (dict(sinks=-1), RuntimeError),
+            (dict(max_new=-1), RuntimeError), (dict(window=2 ** 31), ValueError), (dict(out=h(3, 4, 64).float()), ValueError), (dict(q=h(3, 5, 64)), RuntimeError),
+            (dict(k_cache=h(5, 2, 24, 64), v_cache=h(5, 2, 24, 64)), RuntimeError), (dict(q=h(3, 4, 32), k_cache=h(5, 2, 16, 32), v_cache=h(5, 2, 16, 32)), RuntimeError),
+            (dict(q=z(3, 4, 64, t=torch.float64)), ValueError), (dict(q=h(3 * 4 * 64 + 1)[1:].view(3, 4, 64)), RuntimeError)]),
+    ]
+
+
+def test_refusals():
+    """Wrong types, sizes, strides, devices and values raise before anything is enqueued."""
+    from paper_2411_19379_amd import attention as attn
+    for name, good, cases in _refused():
+        getattr(attn, name)(**good)
+        for kw, error in cases:
+            with pytest.raises(error):
+                getattr(attn, name)(**dict(good, **kw))
 
 
 @pytest.mark.parametrize("in_place", [False, True])
