@@ -1053,7 +1053,7 @@ constexpr int kMostFewRows = 32;
 struct Launch {
     int rows;             // per tile
     uint32_t target;
-    int min_steps;
+    int min_steps, half_steps;
     int64_t most_tiles;   // of all sequences, per key head
     int64_t grid, join_grid, join_units, join_rows, join_blocks, parts, rows_cap;
     size_t bytes;         // of workspace
@@ -1064,16 +1064,17 @@ struct Choice {
     int row_blocks;       // of the kernel for few rows
 };
 
-Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32_t target, int min_steps)
+Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32_t target, int min_steps, int half_steps)
 {
     Launch c;
     const int64_t group = s.n_q_heads / s.n_kv_heads, all_rows = T * group, seqs = batch < T ? batch : T;
     c.rows = rows;
     c.target = ATTN_TARGET ? (uint32_t)(ATTN_TARGET) : target;
     c.min_steps = ATTN_TARGET ? 1 : min_steps;
+    c.half_steps = half_steps;
     c.most_tiles = all_rows / rows + seqs;
-    // A tile of a sequence of n steps has at most ceil(n / per) <= n / per + 1 splits, and the sum of n / per over the tiles is at
-    // most the target.  Only sequences with n > per are split, whose ceil is at most 2 n / per.
+    // A tile of a sequence of n steps has at most n / per + 1 / 2 splits, and the sum of n / per over the tiles is at most the target.
+    // Only sequences with n >= 3 per / 2 are split.
     c.grid = ((c.target + s.n_kv_heads - 1) / s.n_kv_heads + c.most_tiles) * s.n_kv_heads;
     c.parts = 2 * (int64_t)c.target;
     c.rows_cap = rows < all_rows ? rows : all_rows;
@@ -1101,18 +1102,21 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
     c.row_blocks = 1;
     c.chunk = false;
     if (s.io_dtype == ATTN_DT_F32) {
-        c.launch = make_launch(s, batch, T, kF32Rows, 512, 16);
+        c.launch = make_launch(s, batch, T, kF32Rows, 1024, 10, 32);  // (a prompt of 2000 tokens 127 us, shared by 512 137)
     } else if (rows <= kMostFewRows) {
         c.row_blocks = rows <= 16 ? 1 : 2;
-        c.launch = make_launch(s, batch, T, 16 * c.row_blocks, 768, 4);
+        // Many small pieces balance long batches, but each costs the wait for its first keys and a partial result: 64 requests over 512 to
+        // 8192 keys 136 us (shared by 512 workgroups 145), 32 with a single key head 32 us, 16 of up to 5 tokens 30 (always by 1024 37, 34).
+        c.launch = make_launch(s, batch, T, 16 * c.row_blocks, 1024, 4, 24);
     } else {
         c.chunk = true;
-        c.launch = make_launch(s, batch, T, kChunkRows, 256, 8);
+        c.launch = make_launch(s, batch, T, kChunkRows, 256, 6, 0);
     }
     return c;
 }
 
-// The most steps of KT keys that a tile of `rows` rows can have in a table of this width: no more than min_steps are never split.
+// The most steps of KT keys that a tile of `rows` rows can have in a table of this width: fewer than one and a half times
+// min_steps are never split.
 template <int KT> bool may_split(const AttendArgs &a, const Launch &c)
 {
     int64_t steps = ((((int64_t)a.max_blocks << a.log2_bs) + KT - 1) / KT);
@@ -1120,7 +1124,7 @@ template <int KT> bool may_split(const AttendArgs &a, const Launch &c)
         const int64_t seen = ((int64_t)a.window + c.rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
         steps = seen < steps ? seen : steps;
     }
-    return steps > c.min_steps;
+    return steps + c.min_steps / 2 >= 2 * (int64_t)c.min_steps;
 }
 
 template <typename E, int D> hipError_t join(const AttendArgs &a, const Launch &c, bool few, bool f32, hipStream_t stream)
@@ -1232,6 +1236,7 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.most_parts = (int)u.parts;
     a.target = u.target;
     a.min_steps = u.min_steps;
+    a.half_steps = u.half_steps;
     if (s.io_dtype == ATTN_DT_F32)
         return s.head_dim == 64 ? launch_f32<64>(a, u, stream) : launch_f32<128>(a, u, stream);
     if (s.io_dtype == ATTN_DT_BF16)

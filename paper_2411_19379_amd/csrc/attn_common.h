@@ -103,6 +103,7 @@ struct AttendArgs {
     int32_t most_parts;     // partial results there is room for
     uint32_t target;        // workgroups that keep the GPU busy
     int32_t min_steps;      // a workgroup gets no fewer steps of keys than this if it can help it
+    int32_t half_steps;     // up to so many it gets what it would get if half of the workgroups shared them
 };
 
 // ---------------------------------------------------------------- sequences
@@ -201,8 +202,10 @@ struct SeenTiles {
 // ---------------------------------------------------------------- who does what
 // The rows of a sequence are cut into tiles of ROWS rows.  With `per` the steps of a workgroup if the GPU's `target` workgroups
 // shared all steps, the tiles at a sequence's front that take no more than `per` stay whole, and the keys of all others are cut
-// into the same number of splits (a prompt of 2000 tokens 110 us with every tile of it cut, 58 with the long ones).  Every
-// workgroup finds its own piece from the lengths: nothing is planned ahead, so the lengths may change between replays of a graph.
+// into the same number of splits, of about `per` steps if the tile is the last.  (2 requests of 100 and 300 tokens over 1000 to
+// 4000 keys 41 us, with the number of splits rounded up 53; a prompt of 2000 tokens 110 us with every tile of it cut, 60 with the
+// long ones.)  Every workgroup finds its own piece from the lengths: nothing is planned ahead, so the lengths may change between
+// replays of a graph.
 struct Item {
     int seq, tile, split, n_splits;
     int part;  // partial result: split s of key head h of this tile is (part + s) * Hkv + h
@@ -246,6 +249,11 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
         work = sat_add(work, wave_sat_sum(w));
     }
     uint32_t per = work / a.target + (work % a.target != 0);  // steps of a workgroup
+    if (a.half_steps > 0) {
+        const uint32_t half = a.target / 2, twice = work / half + (work % half != 0), most = a.half_steps;
+        const uint32_t least = twice < most ? twice : most;
+        per = per < least ? least : per;
+    }
     per = per < (uint32_t)a.min_steps ? (uint32_t)a.min_steps : per;
 
     int items_before = 0, parts_before = 0;
@@ -255,7 +263,7 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
         int splits[PER], whole[PER], items = 0, parts = 0;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            splits[u] = (int)(((uint32_t)steps[u] + per - 1) / per);
+            splits[u] = (int)(((uint32_t)steps[u] + per / 2) / per);
             whole[u] = splits[u] > 1 ? whole_tiles<ROWS, KT>(a, seq[u], tiles[u], per) : tiles[u];
             const int cut = tiles[u] - whole[u];
             items += of_join ? cut : whole[u] + cut * splits[u];
