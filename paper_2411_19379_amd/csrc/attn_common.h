@@ -113,17 +113,17 @@ struct Seq {
     int cached;
     int rows;    // n * group: the row of token i and the group's head h is i * group + h
 };
-__device__ __forceinline__ Seq load_seq(const AttendArgs &a, int b)
+__device__ __forceinline__ Seq make_seq(const AttendArgs &a, int cu0, int cu1, int cached)
 {
     Seq s;
-    const int64_t from = a.cu[b] < 0 ? 0 : a.cu[b], to = a.cu[b + 1] > a.T ? a.T : a.cu[b + 1];
-    s.start = (int)from;
-    s.n = to > from ? (int)(to - from) : 0;
-    const int c = a.cached[b];
-    s.cached = c < 0 ? 0 : c > 0x3fffffff ? 0x3fffffff : c;
+    const int most = (int)a.T, from = cu0 < 0 ? 0 : cu0, to = cu1 > most ? most : cu1;
+    s.start = from;
+    s.n = to > from ? to - from : 0;
+    s.cached = cached < 0 ? 0 : cached > 0x3fffffff ? 0x3fffffff : cached;
     s.rows = s.n * a.group;
     return s;
 }
+__device__ __forceinline__ Seq load_seq(const AttendArgs &a, int b) { return make_seq(a, a.cu[b], a.cu[b + 1], a.cached[b]); }
 
 // Keys behind the end of the table's rows do not exist.
 __device__ __forceinline__ int table_end(const AttendArgs &a)
@@ -158,14 +158,11 @@ template <int KT> __device__ __forceinline__ KeyRange key_range(const AttendArgs
     return k;
 }
 // How many steps the splits of a sequence are made for: those of its longest tile of rows, but for keys that the table has no
-// place for.  The host computes the same bound for any sequence (may_split).
-template <int KT> __device__ __forceinline__ int most_steps(const AttendArgs &a, const Seq &s, int rows)
+// place for, and no more than a window has.  The host computes the same bounds for any sequence (may_split).
+template <int KT> __device__ __forceinline__ int window_steps(const AttendArgs &a, int rows)
 {
-    const int most = table_end(a), all = ((s.cached + s.n < most ? s.cached + s.n : most) - 1) / KT + 1;
-    if (a.window <= 0)
-        return all;
     const int64_t near = ((int64_t)a.window + rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
-    return near < all ? (int)near : all;
+    return a.window > 0 && near < 0x7fffffff ? (int)near : 0x7fffffff;
 }
 
 __device__ __forceinline__ bool sees(const AttendArgs &a, int pos, int j)
@@ -210,31 +207,31 @@ struct Item {
     int seq, tile, split, n_splits;
     int part;  // partial result: split s of key head h of this tile is (part + s) * Hkv + h
 };
-// How many of a sequence's first tiles take no more than `per` steps.  (With a window the steps hardly depend on the tile.)
-template <int ROWS, int KT> __device__ __forceinline__ int whole_tiles(const AttendArgs &a, const Seq &s, int tiles, uint32_t per)
-{
-    if (a.window > 0)
-        return 0;
-    const int64_t rows = ((int64_t)per * KT - s.cached) * a.group;  // those that see no key behind per * KT
-    return rows <= 0 ? 0 : rows >= s.rows ? tiles : (int)(rows / ROWS);
-}
-
 // The `unit`-th (tile, split) of the launch, or with `of_join` the unit-th tile of the sequences that are split; false if there is
 // none.  Every wave finds out for itself, PER sequences per lane at a time: no barrier, one trip to memory for up to 64 PER
 // sequences.  (With a sequence per thread, sums through LDS and its barriers it was 2.5 us of every workgroup's time.)
 template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(const AttendArgs &a, int unit, bool of_join, Item *out)
 {
     constexpr int ALL = 64 * PER;
-    const int l = lane_id();
-    Seq seq[PER];
-    int tiles[PER], steps[PER];
+    const int l = lane_id(), most_keys = table_end(a), most = window_steps<KT>(a, ROWS);
+    int n[PER], cached[PER], tiles[PER], steps[PER];
+    // no branch in it: all lengths are requested at once
     auto load = [&](int b0) __attribute__((always_inline)) {
+        int from[PER + 1];
+#pragma unroll
+        for (int u = 0; u <= PER; ++u) {
+            const int b = b0 + l * PER + u, at = b < a.batch ? b : a.batch;
+            from[u] = a.cu[at];
+            if (u < PER)
+                cached[u] = a.cached[at < a.batch ? at : a.batch - 1];
+        }
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            const int b = b0 + l * PER + u;
-            seq[u] = load_seq(a, b < a.batch ? b : a.batch - 1);
-            tiles[u] = b < a.batch ? (seq[u].rows + ROWS - 1) / ROWS : 0;
-            steps[u] = tiles[u] > 0 ? most_steps<KT>(a, seq[u], ROWS) : 0;
+            const Seq s = make_seq(a, from[u], from[u + 1], cached[u]);
+            n[u] = s.n, cached[u] = s.cached;
+            tiles[u] = (s.rows + ROWS - 1) / ROWS;
+            const int keys = s.cached + s.n < most_keys ? s.cached + s.n : most_keys, all = (keys - 1) / KT + 1;
+            steps[u] = s.n == 0 ? 0 : all < most ? all : most;
         }
     };
     uint32_t work = 0;  // steps of all workgroups
@@ -264,7 +261,10 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
             splits[u] = (int)(((uint32_t)steps[u] + per / 2) / per);
-            whole[u] = splits[u] > 1 ? whole_tiles<ROWS, KT>(a, seq[u], tiles[u], per) : tiles[u];
+            // of the first tiles, that take no more than `per` steps; with a window the steps hardly depend on the tile
+            const int keys = (int)(((uint32_t)steps[u] < per ? (uint32_t)steps[u] : per) * KT - (uint32_t)cached[u]);
+            const int short_tiles = a.window > 0 || keys <= 0 ? 0 : keys >= n[u] ? tiles[u] : keys * a.group / ROWS;
+            whole[u] = splits[u] > 1 ? short_tiles : tiles[u];
             const int cut = tiles[u] - whole[u];
             items += of_join ? cut : whole[u] + cut * splits[u];
             parts += cut * splits[u];
