@@ -1083,10 +1083,11 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32
     c.join_blocks = (c.rows_cap + c.join_rows - 1) / c.join_rows;
     c.join_units = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * c.join_blocks;
     c.join_grid = c.join_units < kJoinWorkgroups ? c.join_units : kJoinWorkgroups;
-    // One sequence with tiles for all the workgroups that are wanted is split only if it has fewer tokens than there are rows: a few
-    // workgroups are enough to find nothing to do (a prompt of 2000 tokens 60.9 us, with the usual number of them 63.2).
-    if (batch == 1 && (all_rows + rows - 1) / rows * s.n_kv_heads >= c.target && c.join_grid > 64)
-        c.join_grid = 64;
+    // Where there is a tile for every workgroup that is wanted, only tiles of far more steps than the others are cut: hardly anything to
+    // join as a rule, and a few workgroups find that out sooner (256 requests of one token with a window 149 us, by 2048 153; 16
+    // packed prompts 306, 309; but where most tiles are cut 64 requests of one token 143, 136).
+    if (c.most_tiles * s.n_kv_heads >= c.target && c.join_grid > 256)
+        c.join_grid = 256;
     c.bytes = (size_t)(c.parts * c.rows_cap) * (s.head_dim + 2) * sizeof(float);
     return c;
 }
