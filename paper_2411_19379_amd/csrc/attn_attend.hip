@@ -37,6 +37,11 @@ template <typename E> __device__ __forceinline__ void unpack4(uint2 u, float *v)
 // half one phase later.  V(t + 1) and K(t + 2) are requested at the start of a wave's softmax t, phase 2t + 1 or 2t + 2, behind
 // the last reads of what they replace, V(t - 2) and K(t - 1) in phase 2t - 1; a wave waits for what it has requested at the end
 // of its products t + 1, phase 2t + 2 or 2t + 3, and the first reads are in phase 2t + 4.
+//
+// With 128 values per head a tile of a wave is 1024 cycles of products and about 870 of softmax: the matrix cores bind, at the
+// clock that the power allows (32768 tokens over 16384 cached, 32 heads, bf16: 15.0 ms, 1170 TFLOP/s, matrix cores busy 62 % of
+// the cycles at 1.8 GHz).  With 64 the products are half as many and the softmax the same, which binds (16 packed prompts of 512
+// to 4096 tokens, 16 heads, fp16: 316 us, 620 TFLOP/s).  A tile of 256 rows by 64 keys needs 32 KB from the L2 for some 2 us.
 constexpr int kChunkKeys = 64;
 
 constexpr int kChunkBuffers = 3;
@@ -106,7 +111,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
 
     // What this wave moves: KEYS neighbouring keys, of V of one tile and of K of the next; this lane piece load_at of its rows,
     // from where that piece of the row is.  With WIDE, blocks of at least KEYS keys, they lie in one block: one scalar look-up,
-    // uniform addresses (32768 tokens over 16384 cached: 16.4 ms, with a look-up and an address per lane 18.6).  A key that does
+    // uniform addresses (32768 tokens over 16384 cached 16.4 ms against 18.6 with a look-up and an address per lane).  A key that does
     // not exist is read from the cache's first rows, so that no load waits for a branch: what it gets as K comes to nothing in
     // the softmax, as V it is cleared.
     const int load_row = wave * KEYS + l / PIECES, load_at = l % PIECES;
@@ -407,7 +412,9 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
 // ================================================================ few rows
 // For the rows of single tokens, 16 RB of them at a time: each of the four waves takes every fourth tile of 32 keys, K from
 // memory right into the operand's registers, V through LDS of its own for the transposing reads; no barriers until the waves'
-// results are joined.  What bounds it is reading the cache: a wave's next tile is requested before the present one is used.
+// results are joined.  What bounds it is reading the cache, once: a wave's next tile is requested before the present one is used
+// (64 requests over 512 to 8192 keys, 8 key heads of 128, bf16: 136 us, 5.1 TB/s; 256 with a window of 1024: 149 us, 5.1 TB/s, the
+// rate of a large copy).  A single request over 4012 keys is latency: 14 us, 8 of them this kernel and 5 the join.
 constexpr int kFewKeys = 32;
 constexpr int kFewWaves = 4;
 
@@ -468,8 +475,8 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
             o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // With WIDE, blocks of at least 16 keys, a tile's keys lie in two blocks: scalar look-ups, and every load is a uniform address
-    // and an offset that does not change (32 sequences of one token, 32 rows of heads: 114 us, with a look-up per lane 126).  A key that does not exist is read from the cache's first rows: as K it comes to nothing
-    // in the softmax, as V it is cleared.
+    // and an offset that does not change (32 requests of 8 tokens, 32 rows of heads: 114 us, with a look-up per lane 126).  A key
+    // that does not exist is read from the cache's first rows: as K it comes to nothing in the softmax, as V it is cleared.
     const int32_t *const table = a.table + (int64_t)it.seq * a.max_blocks;
     const int bs_mask = (1 << a.log2_bs) - 1;
     const uint32_t k_offset = l % 16 * D * 2 + 16 * quarter, v_offset = l * 16;
@@ -721,7 +728,9 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
 
 // ================================================================ fp32
 // 16 rows per wave, 64 per workgroup, keys in tiles of 32 through LDS in two buffers; products on the fp32 matrix instructions,
-// which bound it (a sixteenth of the 16-bit rate).
+// which take 2048 cycles of a wave's 4000 to 5100 per tile with heads of 64 (a sixteenth of the 16-bit rate): 3 packed prompts of
+// 1537 tokens with a window of 300, 16 heads of 64, 38 us, 48 TFLOP/s; a prompt of 2000 tokens 126 us, 65 TFLOP/s.  Keys from
+// two tiles ahead, in registers, and addresses from scalar look-ups changed nothing.
 constexpr int kF32Keys = 32;
 constexpr int kF32Waves = 4;
 
@@ -732,6 +741,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     constexpr int STRIDE = D + 4;  // floats; rows four apart start 16 banks apart
     extern __shared__ __align__(16) unsigned char lds_raw[];
     constexpr int TILE = kF32Keys * STRIDE;
+    constexpr int kAhead = 6;      // reads of V
     float *const lds_k = reinterpret_cast<float *>(lds_raw), *const lds_v = lds_k + 2 * TILE;
     int *const lds_flag = reinterpret_cast<int *>(lds_v + 2 * TILE);  // [2][32]: bit 0 the key exists, bit 1 its V is not finite
 
@@ -794,6 +804,10 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         request(step_begin);
         look_up(step_begin + 1);
     }
+    // q is waited for here: a wait for it in the loop would be one for the next tile's loads as well
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+        qf[ks] = unknown(qf[ks]);
     const SeenTiles seen_tiles(a, keys.pos0, keys.pos1, kF32Keys);
     for (int step = step_begin; step < step_end; ++step) {
         const int j0 = keys.tile(step) * kF32Keys;
@@ -889,6 +903,14 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 #pragma unroll
                 for (int db = 0; db < D / 16; ++db)
                     o[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[(kb * 16 + 4 * quarter + r) * STRIDE + db * 16 + l % 16], st[kb][r], o[db], 0, 0, 0);
+        // the reads of V (two of them in an instruction) run ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+            if (i + kAhead < D / 4)
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
         for (uint32_t left = bad; left != 0; left &= left - 1) {
             const int key = __builtin_ctz(left), e_of = 4 * (key / 16) + key % 4, from = key % 16 / 4;
             const int e = (j0 + key) >> a.log2_bs, cr = cache_row(a, j0 + key < end && e < a.max_blocks ? table[e] : -1, kv_head, j0 + key);
@@ -940,7 +962,9 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 
 // ================================================================ joining
 // The rows of sequences whose keys were split, a wave per row: the lanes load the maxima and weights of up to 64 parts at once,
-// then the sums in the order of the parts, 64 * 4 / D parts per load and kJoinAhead loads on their way.
+// then the sums in the order of the parts, 64 * 4 / D parts per load and kJoinAhead loads on their way.  Two dependent trips to
+// memory bound it (a chat turn's 4384 rows of 10 parts: 10 us; two rows per wave at once were 2 us faster there and 4 us slower
+// for few rows of many parts).
 constexpr int kJoinThreads = 256;
 constexpr int kJoinAhead = 4;
 constexpr int kJoinWorkgroups = 2048;

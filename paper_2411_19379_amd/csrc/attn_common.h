@@ -45,7 +45,7 @@ __device__ __forceinline__ void memory_wait() { asm volatile("s_waitcnt vmcnt(0)
 
 // The value, of which the compiler knows nothing: what rare branches compute from it stays in them instead of taking registers
 // of the loops around them.
-__device__ __forceinline__ int unknown(int v)
+template <typename T> __device__ __forceinline__ T unknown(T v)
 {
     asm volatile("" : "+v"(v));
     return v;

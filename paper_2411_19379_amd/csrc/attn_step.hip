@@ -9,7 +9,7 @@ namespace {
 // the blocks of sequence b start at the sum of the needs in front of it.  Every workgroup computes these sums for itself
 // (a batch is a few KiB of lengths), then the workgroups deal with disjoint tokens and disjoint rows of the table.  Small
 // calls are all latency: one launch, and what a workgroup reads of global memory are the lengths and, per token, one table
-// entry or one free block.
+// entry or one free block (a chat turn 8 us per call, 2.8 of them in the kernel; 256 requests of up to 512 tokens 8 us, 7.3).
 constexpr int kAssignThreads = 256;
 constexpr int kAssignTokens = 4;  // per thread
 
@@ -141,7 +141,8 @@ __global__ __launch_bounds__(kAssignThreads) void attn_assign_kernel(AssignArgs 
 
 // ---------------------------------------------------------------- rotary positions and the append
 // Streaming: every value of q, k and v is read and written once.  A thread takes 8 values of v, or of a part of a head that
-// does not turn, or 8 pairs of a head of q or k (two runs of 8 values in the half layout, one of 16 interleaved).
+// does not turn, or 8 pairs of a head of q or k (two runs of 8 values in the half layout, one of 16 interleaved).  Memory bounds
+// it: 32768 tokens of 32 + 8 + 8 heads of 128 in bf16 142 us, 5.8 TB/s; small calls are a launch (64 tokens 8 us, the kernel 3).
 constexpr int kRopeThreads = 256;
 
 struct RopeArgs {
