@@ -1095,7 +1095,7 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32
     c.rows = rows;
     c.target = ATTN_TARGET ? (uint32_t)(ATTN_TARGET) : target;
     c.min_steps = ATTN_TARGET ? 1 : min_steps;
-    c.half_steps = half_steps;
+    c.half_steps = ATTN_TARGET ? 0 : half_steps;
     c.most_tiles = all_rows / rows + seqs;
     // A tile of a sequence of n steps has at most n / per + 1 / 2 splits, and the sum of n / per over the tiles is at most the target.
     // Only sequences with n >= 3 per / 2 are split.

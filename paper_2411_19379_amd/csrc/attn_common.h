@@ -252,6 +252,7 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
         per = per < least ? least : per;
     }
     per = per < (uint32_t)a.min_steps ? (uint32_t)a.min_steps : per;
+    per = work == 0xffffffffu ? 0x7fffffffu : per;  // a sum that did not fit says nothing but that there are tiles enough
 
     int items_before = 0, parts_before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += ALL) {
@@ -359,8 +360,6 @@ template <typename E> __device__ __forceinline__ bool drop_not_finite(uint32_t &
     u = (lo ? 0u : u & 0xffffu) | (hi ? 0u : u & 0xffff0000u);
     return lo || hi;
 }
-
-__device__ __forceinline__ bool not_finite(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
 // p v where v is not finite and the row sees its key (sees: all bits, or none), else 0, without a condition register.
 __device__ __forceinline__ float not_finite_part(float p, float v, uint32_t sees)
