@@ -118,6 +118,48 @@ def test_attend_long(name):
     ah.check(p, *_attend(p), name, ref=_reference64(p))
 
 
+# One long sequence among many short ones: a tile for every workgroup, and some of them cut into many pieces all the same.
+SKEWED = {
+    "chunks": (8, 8, 64, 16, "bf16", [200] * 40 + [100] + [30] * 5, [7] * 20 + [0] * 20 + [20000] + [64] * 5, 0, 0, 0),
+    "chunks_hint": (8, 8, 128, 32, "f16", [20] * 64 + [17], [100] * 64 + [20000], 0, 0, 20),
+    "tokens": (4, 4, 128, 16, "bf16", [1] * 300, [10 + i % 50 for i in range(299)] + [40000], 0, 0, 1),
+    "tokens_window": (4, 4, 64, 16, "f16", [1] * 300, [10 + i % 50 for i in range(299)] + [40000], 3000, 5, 1),
+    "f32": (8, 8, 64, 16, "f32", [60] * 130 + [3], [7] * 130 + [9000], 0, 0, 0),
+}
+
+
+@pytest.mark.parametrize("name", sorted(SKEWED))
+def test_attend_one_long_sequence_among_many(name):
+    print(f"attend skewed {name}", flush=True)
+    p = ah.make(23, *SKEWED[name])
+    ah.check(p, *_attend(p), name, ref=_reference64(p))
+
+
+def _random(seed):
+    rs = np.random.RandomState(seed)
+    hkv, group = int(rs.choice([1, 2, 3, 8])), int(rs.choice([1, 2, 3, 4, 7, 16, 33]))
+    batch, longest = int(rs.choice([1, 2, 5, 17, 70])), int(rs.choice([1, 1, 4, 40, 400]))
+    new = [int(rs.randint(0, longest + 1)) for _ in range(batch)]
+    new[int(rs.randint(batch))] = longest
+    cached = [int(rs.choice([0, 1, 15, 16, 63, 64, 65, int(rs.randint(0, 900)), int(rs.randint(0, 4000))])) for _ in range(batch)]
+    window = int(rs.choice([0, 0, 1, 31, 200, 1000]))
+    return (group * hkv, hkv, int(rs.choice([64, 128])), int(rs.choice([1, 2, 4, 8, 16, 32, 64, 256])), str(rs.choice(["f32", "bf16", "f16"])), new, cached,
+            window, int(rs.choice([0, 1, 5, 40])) if window else 0, int(rs.choice([0, longest])))
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_attend_random(seed):
+    """Heads, lengths, blocks, types, windows and hints at random, a tenth of the blocks missing in every third problem; the
+    same call once more gives the same bits."""
+    case = _random(seed)
+    print(f"attend random {seed}: {case[:5]} batch {len(case[5])}, {sum(case[5])} new, window {case[7:]}", flush=True)
+    p = ah.make(seed, *case, holes=0.1 if seed % 3 == 0 else 0.0)
+    got = _attend(p)
+    ah.check(p, *got, str(case), ref=_reference64(p))
+    again = _attend(p)
+    assert np.array_equal(got[0], again[0]) and np.array_equal(got[1], again[1], equal_nan=True)
+
+
 def test_attend_rows_of_a_projection_on_another_stream():
     """q is a part of wider rows, out as well; the call goes to the stream that is current."""
     from paper_2411_19379_amd import attention as attn
