@@ -117,13 +117,14 @@ CASES = {
 }
 
 
-@pytest.mark.parametrize("target", [0, 60])
-@pytest.mark.parametrize("name", sorted(CASES))
+@pytest.mark.parametrize("name,target", [(name, 60) for name in sorted(CASES)] + [(name, 2) for name in sorted(CASES)] +
+                         [(name, 0) for name in ("chunk_group", "decode", "f32", "few_tokens", "few_tokens_wide")])
 def test_attend(emu, tmp_path, name, target):
     p = ah.make(11, *CASES[name])
     out, lse = _attend(emu, tmp_path, p, target=target)
     ah.check(p, out, lse, name)
-    for order, side, late in ((1, "start", 1), (5, "end", 0), (4, "end", 1)):
+    # (most of the workgroups of target 0, the one that is used, have nothing to do)
+    for order, side, late in ((1, "start", 1), (5, "end", 0), (4, "end", 1)) if target else ((5, "start", 1),):
         other = _attend(emu, tmp_path, p, order, side, target, late=late)
         assert np.array_equal(out, other[0]) and np.array_equal(lse, other[1]), f"{name}: order {order} changes the result"
 
@@ -135,7 +136,7 @@ def test_attend_with_blocks_missing(emu, tmp_path, name):
     p = ah.make(5, *case, holes=0.5)
     if name == "decode":
         p.table[0] = -1
-    for target in (0, 40):
+    for target in (2, 40):
         out, lse = _attend(emu, tmp_path, p, target=target, gap=16)
         ah.check(p, out, lse, name)
     if name == "decode":
@@ -148,7 +149,7 @@ def test_attend_with_a_table_that_is_too_narrow(emu, tmp_path, name):
     p = ah.make(13, *CASES[name])
     for width in (1, 3):
         p.table = np.ascontiguousarray(ah.make(13, *CASES[name]).table[:, :width])
-        for target in (0, 40):
+        for target in (2, 40):
             out, lse = _attend(emu, tmp_path, p, target=target)
             ah.check(p, out, lse, f"{name} {width}")
 
@@ -169,7 +170,7 @@ def test_attend_not_finite_stays_with_the_rows_that_see_it(emu, tmp_path, name, 
             if 0 <= j < total:
                 block, row = p.block_row(seq, j)
                 cache[block, i % p.hkv, row, (5 * i + j) % p.d] = bad
-    for target in (0, 30):
+    for target in (2, 30):
         out, lse = _attend(emu, tmp_path, p, target=target)
         ah.check(p, out, lse, name)
 
@@ -186,7 +187,7 @@ def test_attend_scores_of_minus_infinity_alone(emu, tmp_path):
                     p.k_cache[block, 0, row] = -float("inf")
         for max_new in (0, 1):
             p.max_new = max_new
-            for target in (0, 9):
+            for target in (2, 9):
                 out, lse = _attend(emu, tmp_path, p, target=target)
                 assert np.isnan(out[0]).all() and np.isfinite(out[71]).all()
                 ah.check(p, out, lse, f"{dtype} {max_new} {target}")
@@ -202,7 +203,7 @@ def test_attend_large_scores(emu, tmp_path):
                     block, row = p.block_row(b, j)
                     p.k_cache[block, 0, row, 0] = 0.5 * j
             p.q[:, :, 0] = 40.0
-            out, lse = _attend(emu, tmp_path, p)
+            out, lse = _attend(emu, tmp_path, p, target=20)
             ah.check(p, out, lse, dtype, sums=0.0 if dtype != "f32" else 40.0 * 0.5 * 200 * p.scale)
 
 
@@ -222,11 +223,10 @@ def many(name):
     return ah.make(17, hq, hkv, d, bs, dtype, [int(n) for n in new], *rest)
 
 
-@pytest.mark.parametrize("target", [0, 900])
 @pytest.mark.parametrize("name", sorted(MANY))
-def test_attend_many_sequences(emu, tmp_path, name, target):
+def test_attend_many_sequences(emu, tmp_path, name):
     p = many(name)
-    ah.check(p, *_attend(emu, tmp_path, p, target=target), name)
+    ah.check(p, *_attend(emu, tmp_path, p, target=400), name)
 
 
 # heads, key heads, head_dim, block size, type, new tokens (the last ones belong to no sequence), cached tokens
@@ -257,7 +257,7 @@ def check_padded(p, out, lse, what):
     ah.check(p, out[:n], lse[:n], what, ref=[x[:n] for x in ah.reference(p)])
 
 
-@pytest.mark.parametrize("target", [0, 2, 30])
+@pytest.mark.parametrize("target", [2, 30])
 @pytest.mark.parametrize("name", sorted(PADDED))
 def test_attend_rows_of_no_sequence(emu, tmp_path, name, target):
     """cu_seqlens ends in front of the rows' end, as in a captured step with room for more tokens; a single sequence that has few
@@ -273,7 +273,7 @@ def test_attend_widest_window(emu, tmp_path, name):
     ref = ah.reference(p)
     for window, sinks in ((2 ** 31 - 1, 0), (2 ** 31 - 1, 2 ** 31 - 1), (1, 2 ** 31 - 1)):
         p.window, p.sinks = window, sinks
-        for target in (0, 40):
+        for target in (2, 40):
             ah.check(p, *_attend(emu, tmp_path, p, target=target), f"{name} {window} {sinks}", ref=ref)
 
 
