@@ -46,19 +46,23 @@ __device__ __forceinline__ AssignSeq assign_seq(const AssignArgs &a, int b)
 // The order-th block that the call hands out.
 __device__ __forceinline__ int free_block(const AssignArgs &a, int n_free, int64_t order)
 {
-    return order < n_free ? a.free_blocks[n_free - 1 - order] : -1;
+    return (uint64_t)order < (uint64_t)n_free ? a.free_blocks[n_free - 1 - order] : -1;
 }
+// Sums of needs take 64 bits: the needs of sequences that name the same tokens again and again exceed 32.  wave_scan of values up
+// to 2^31, in halves of 16 bits, whose sums over a wave fit.
+__device__ __forceinline__ int64_t wave_scan64(int v) { return ((int64_t)wave_scan(v >> 16) << 16) + wave_scan(v & 0xffff); }
+__device__ __forceinline__ int sat32(int64_t v) { return v > 0x7fffffff ? 0x7fffffff : (int)v; }
 
 __global__ __launch_bounds__(kAssignThreads) void attn_assign_kernel(AssignArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds_raw[];
     int *start = reinterpret_cast<int *>(lds_raw);        // [batch] first token of each sequence, at least the one in front
-    int *base = start + a.batch;                          // [batch] blocks handed out in front of it
-    int *sums = base + a.batch;                           // [8]
+    int *base = start + a.batch;                          // [batch] blocks handed out in front of it, 2^31 - 1 if more
+    int64_t *sums = reinterpret_cast<int64_t *>(base + a.batch);  // [4]
     const int tid = threadIdx.x, wave = tid / 64, l = lane_id();
     int n_free = *a.n_free;
     n_free = n_free < 0 ? 0 : n_free > a.free_capacity ? a.free_capacity : n_free;
-    int before = 0;
+    int64_t before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kAssignThreads) {
         const int b = b0 + tid;
         int need = 0;
@@ -67,25 +71,25 @@ __global__ __launch_bounds__(kAssignThreads) void attn_assign_kernel(AssignArgs 
             need = s.need();
             start[b] = s.start;
         }
-        const int upto = wave_scan(need);
+        const int64_t upto = wave_scan64(need);
         lds_barrier();
         if (l == 63)
             sums[wave] = upto;
         lds_barrier();
-        int mine = before + upto - need;
+        int64_t mine = before + upto - need;
         for (int w = 0; w < kAssignThreads / 64; ++w) {
             mine += w < wave ? sums[w] : 0;
             before += sums[w];
         }
         if (b < a.batch)
-            base[b] = mine;
+            base[b] = sat32(mine);
     }
     lds_barrier();
     const int bs = 1 << a.log2_bs;
     if ((int)blockIdx.x < a.token_workgroups) {
         if (blockIdx.x == 0 && tid == 0) {
-            a.counts[0] = before < n_free ? n_free - before : 0;
-            a.counts[1] = before > n_free ? before - n_free : 0;
+            a.counts[0] = before < n_free ? (int)(n_free - before) : 0;
+            a.counts[1] = before > n_free ? sat32(before - n_free) : 0;
         }
 #pragma unroll 1
         for (int u = 0; u < kAssignTokens; ++u) {
@@ -302,7 +306,7 @@ hipError_t launch_attn_assign(int batch, int log2_bs, int max_blocks, int64_t T,
     const int64_t per = kAssignThreads * kAssignTokens;
     a.token_workgroups = (int)(T > 0 ? (T + per - 1) / per : 1);  // the first one also writes the counts
     a.table_workgroups = batch < 256 ? batch : 256;
-    const size_t lds = (2 * (size_t)batch + 8) * sizeof(int);
+    const size_t lds = 2 * (size_t)batch * sizeof(int) + kAssignThreads / 64 * sizeof(int64_t);
     hipLaunchKernelGGL(attn_assign_kernel, dim3((unsigned)(a.token_workgroups + a.table_workgroups)), dim3(kAssignThreads), lds,
                        stream, a);
     return hipGetLastError();

@@ -1,0 +1,108 @@
+"""Index arrays that no caller should pass: lengths that decrease, are negative or reach behind the arrays, sequences that name the
+same tokens, blocks and positions of nowhere.  Every buffer of the emulation lies against inaccessible pages, so an access
+outside the arguments ends the run; what the operators say of such a call has to make sense all the same."""
+import numpy as np
+import pytest
+
+import attn_helpers as ah
+from test_attention_emulation import _attend, _run, emu  # noqa: F401
+
+MOST = 2 ** 31 - 1
+
+
+def _assign(exe, tmp_path, bs, T, cu, cached, table, free, n_free, shared=None, in_place=False, **kw):
+    cu, cached, table, free = (np.array(x, np.int32) for x in (cu, cached, table, free))
+    batch, width = table.shape
+    raw = _run(exe, tmp_path, 0, [batch, bs.bit_length() - 1, width, T, shared is not None, len(free), in_place],
+               [cu, cached, *([np.array(shared, np.int32)] if shared is not None else []), table, free, np.array([n_free], np.int32)], **kw)
+    got = []
+    for t, shape in ((np.int32, (batch, width)), (np.int64, T), (np.int32, T), (np.int32, (batch, 4)), (np.int32, 2)):
+        n = int(np.prod(shape)) * t().itemsize
+        got.append(np.frombuffer(raw[:n], t).reshape(shape))
+        raw = raw[n:]
+    return got
+
+
+def test_assign_needs_beyond_32_bits(emu, tmp_path):
+    """2048 sequences that all name the same tokens: their needs add up to more than 2^31."""
+    batch, T, free = 4096, 2 ** 20 + 4096, np.arange(100, 116)
+    cu = np.array([0 if b % 2 == 0 else T for b in range(batch + 1)])
+    table, slots, positions, copies, counts = _assign(emu, tmp_path, 1, T, cu, np.zeros(batch), np.full((batch, 2), -1), free, 16)
+    assert counts.tolist() == [0, MOST]
+    assert set(np.unique(table)) <= {-1, *free} and set(np.unique(slots)) <= {-1, *free}
+    given = table[table >= 0]
+    assert len(set(given)) == len(given) and np.all(copies[:, :2] == -1)
+
+
+# cu_seqlens, cached_lens; 40 tokens
+LENGTHS = {
+    "decreasing": ([0, 30, 10, 40], [5, 0, 9]),
+    "negative": ([-7, -3, 12, 40], [-5, 3, -2 ** 31]),
+    "behind_the_end": ([0, 50, 1000, MOST], [5, 4, 3]),
+    "far_behind": ([MOST, MOST, 0, 40], [MOST, MOST, MOST]),
+    "late_start": ([9, 9, 20, 38], [1, 2, 3]),
+    "long_cached": ([0, 10, 20, 40], [MOST, 2 ** 30, 100000]),
+    "all_the_same": ([0, 40, 0, 40], [0, 17, 2]),
+}
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("name", sorted(LENGTHS))
+def test_assign_lengths(emu, tmp_path, name, in_place):
+    cu, cached = LENGTHS[name]
+    held, free = np.arange(18).reshape(3, 6), np.arange(100, 120)
+    for bs in (1, 8):
+        for n_free in (-3, 0, 11, 20, MOST):
+            table, slots, positions, copies, counts = _assign(emu, tmp_path, bs, 40, cu, cached, held, free, n_free, shared=[1, 0, -1],
+                                                              in_place=in_place, side="end" if bs == 1 else "start")
+            most = min(max(n_free, 0), 20)
+            assert 0 <= counts[0] <= most and counts[1] >= 0
+            assert set(np.unique(table)) <= {-1, *held.ravel(), *free}
+            blocks = slots[slots >= 0] // bs
+            assert set(np.unique(blocks)) <= {*held.ravel(), *free} and np.all(slots >= -1) and np.all(positions >= 0)
+            given = table[table >= 100]
+            assert len(set(given)) == len(given) <= most - counts[0]
+
+
+@pytest.mark.parametrize("name", sorted(LENGTHS))
+@pytest.mark.parametrize("case", ["few_window", "chunk_group", "f32"])
+def test_attend_lengths(emu, tmp_path, case, name):
+    """Rows of the arguments alone are written, and read keys come from the cache: a row's results are means of its values."""
+    hq, hkv, d, bs, dtype, _, _, window, sinks, max_new = {
+        "few_window": (3, 3, 64, 4, "bf16", 0, 0, 20, 3, 1), "chunk_group": (4, 1, 64, 16, "f16", 0, 0, 0, 0, 0),
+        "f32": (4, 2, 64, 16, "f32", 0, 0, 0, 0, 0)}[case]
+    p = ah.make(3, hq, hkv, d, bs, dtype, [10, 20, 10], [30, 20, 40], window, sinks, max_new, spare=0)
+    p.k_cache[:] = p.k_cache.nan_to_num(0.0)
+    p.v_cache[:] = p.v_cache.nan_to_num(0.0)
+    most = float(p.v_cache.abs().max()) * (1 + 2.0 ** -7)
+    cu, p.cached = np.array(LENGTHS[name][0], np.int32), LENGTHS[name][1]
+    T = p.T
+    p.cu = cu
+    p.__class__ = type("Cut", (ah.Problem,), {"T": property(lambda self: T)})
+    for target, side in ((2, "end"), (30, "start")):
+        out, lse = _attend(emu, tmp_path, p, target=target, side=side)
+        # rows of no sequence keep the NaN patterns they started with
+        assert np.all(np.isnan(out) | (np.abs(out) <= most))
+        assert not np.any(np.isposinf(lse))
+
+
+def test_append_nowhere(emu, tmp_path):
+    """Slots, positions and copies of nowhere: only what lies in the caches is written."""
+    hq, hkv, d, bs, T, n_blocks, most = 2, 1, 64, 4, 9, 3, 5
+    rs = np.random.RandomState(1)
+    qkv, rotary = rs.randn(T, (hq + 2 * hkv) * d).astype(np.float32), rs.randn(most, 2, 16).astype(np.float32)
+    caches = [rs.randn(n_blocks, hkv, bs, d).astype(np.float32) for _ in "kv"]
+    positions = np.array([-1, 5, MOST, -2 ** 31, 0, 1, 2, 3, 4], np.int32)
+    slots = np.array([-1, 12, 2 ** 40, -2 ** 63, 2 ** 63 - 1, 2 ** 32, 11, -2 ** 32, 0], np.int64)
+    copies = np.array([[0, 3, 4, 0], [-1, 2, 4, 0], [2 ** 31 - 1, 1, 4, 0], [1, -2 ** 31, 4, 0], [1, 2, -9, 0]], np.int32)
+    raw = _run(emu, tmp_path, 1, [hq, hkv, d, bs, 0, T, len(copies), n_blocks, most, 32, 0, 1, (hq + 2 * hkv) * d],
+               [qkv, positions, slots, rotary, copies, *caches])
+    flat = np.frombuffer(raw, np.float32)
+    k, v = flat[T * hq * d:].reshape(2, n_blocks, hkv, bs, d)
+    kept = np.ones((n_blocks, bs), bool)
+    kept[2, 3] = kept[0, 0] = False
+    for got, was, part in ((k, caches[0], 2), (v, caches[1], 3)):
+        assert np.array_equal(got[:, 0][kept], was[:, 0][kept])
+        assert np.array_equal(got[2, 0, 3, 32:], qkv[6].reshape(-1, d)[part, 32:]) and np.array_equal(got[0, 0, 0, 32:], qkv[8].reshape(-1, d)[part, 32:])
+    q = flat[:T * hq * d].reshape(T, hq, d)
+    assert np.isnan(q[:4, :, :32]).all() and np.isfinite(q[4:]).all()
