@@ -92,13 +92,17 @@ typedef struct {
  *   free_blocks  [n_free]   int32 device;  n_free: int32 device, one value,
  *                           at most free_capacity
  *   slots        [total_tokens]  int64 device, out: block * block_size + row,
- *                           or -1 for a token that got no block
+ *                           or -1 for a token that got no block: the free
+ *                           list ran out, or its entry lies behind the end of
+ *                           the table's row (no block is taken for that)
  *   positions    [total_tokens]  int32 device, out
  *   copies       [batch, 4] int32 device, out: from block, to block, rows, 0;
  *                           (-1, -1, 0, 0) where nothing is to be copied.  If the free list
  *                           ran out "to" is -1.
  *   counts       [2]        int32 device, out: blocks left on the free list,
- *                           blocks that were missing.  Must not overlap n_free.
+ *                           blocks that were missing in this call, entries of
+ *                           new tokens behind the end of a row among them.
+ *                           Must not overlap n_free.
  *
  * batch is at most 4096.
  */

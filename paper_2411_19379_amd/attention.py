@@ -107,7 +107,7 @@ class Step(NamedTuple):
     slots: "torch.Tensor"      # [total_tokens] int64, -1: no block
     positions: "torch.Tensor"  # [total_tokens] int32
     copies: "torch.Tensor"     # [batch, 4] int32: from block, to block, rows, 0
-    counts: "torch.Tensor"     # [2] int32: free blocks left, blocks missing
+    counts: "torch.Tensor"     # [2] int32: free blocks left, blocks missing in this call (list empty, or row too short)
 
 
 def assign_blocks(block_size: int, total_tokens: int, cu_seqlens, cached_lens, table, free_blocks, n_free,

@@ -5,11 +5,11 @@
 namespace {
 
 // ---------------------------------------------------------------- blocks, slots, positions
-// need_b = ceil((cached_b + n_b) / bs) - ceil(cached_b / bs), one more where a shared block that is not full is replaced;
-// the blocks of sequence b start at the sum of the needs in front of it.  Every workgroup computes these sums for itself
-// (a batch is a few KiB of lengths), then the workgroups deal with disjoint tokens and disjoint rows of the table.  Small
-// calls are all latency: one launch, and what a workgroup reads of global memory are the lengths and, per token, one table
-// entry or one free block (a chat turn 8 us per call, 2.8 of them in the kernel; 256 requests of up to 512 tokens 8 us, 7.3).
+// need_b = ceil((cached_b + n_b) / bs) - ceil(cached_b / bs), one more where a shared block that is not full is replaced, without
+// entries behind the end of the table's row; the blocks of sequence b start at the sum of the needs in front of it.  Every
+// workgroup computes these sums for itself (a batch is a few KiB of lengths), then the workgroups deal with disjoint tokens and
+// disjoint rows of the table.  Small calls are all latency: one launch, and what a workgroup reads of global memory are the
+// lengths and, per token, one table entry or one free block (a chat turn 8 us per call, 2.8 of them in the kernel; 256 requests of up to 512 tokens 8 us, 7.3).
 constexpr int kAssignThreads = 256;
 constexpr int kAssignTokens = 4;  // per thread
 
@@ -27,7 +27,19 @@ struct AssignSeq {
     int have;   // table entries that stay
     int all;    // entries with the new tokens
     bool fork;  // the last cached block is replaced
-    __device__ __forceinline__ int need() const { return n > 0 ? all - have : 0; }
+    // entries that want a block, of those that the row has
+    __device__ __forceinline__ int need(int max_blocks) const
+    {
+        const int end = all < max_blocks ? all : max_blocks;
+        return n > 0 && end > have ? end - have : 0;
+    }
+    // entries of new tokens that the row does not have
+    __device__ __forceinline__ int behind(const AssignArgs &a) const
+    {
+        const int first = cached >> a.log2_bs;
+        const int from = first > a.max_blocks ? first : a.max_blocks;
+        return n > 0 && all > from ? all - from : 0;
+    }
 };
 __device__ __forceinline__ AssignSeq assign_seq(const AssignArgs &a, int b)
 {
@@ -59,16 +71,19 @@ __global__ __launch_bounds__(kAssignThreads) void attn_assign_kernel(AssignArgs 
     int *start = reinterpret_cast<int *>(lds_raw);        // [batch] first token of each sequence, at least the one in front
     int *base = start + a.batch;                          // [batch] blocks handed out in front of it, 2^31 - 1 if more
     int64_t *sums = reinterpret_cast<int64_t *>(base + a.batch);  // [4]
+    uint32_t *behind_sums = reinterpret_cast<uint32_t *>(sums + kAssignThreads / 64);  // [4]
     const int tid = threadIdx.x, wave = tid / 64, l = lane_id();
     int n_free = *a.n_free;
     n_free = n_free < 0 ? 0 : n_free > a.free_capacity ? a.free_capacity : n_free;
     int64_t before = 0;
+    uint32_t behind = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kAssignThreads) {
         const int b = b0 + tid;
         int need = 0;
         if (b < a.batch) {
             const AssignSeq s = assign_seq(a, b);
-            need = s.need();
+            need = s.need(a.max_blocks);
+            behind = sat_add(behind, (uint32_t)s.behind(a));
             start[b] = s.start;
         }
         const int64_t upto = wave_scan64(need);
@@ -84,12 +99,18 @@ __global__ __launch_bounds__(kAssignThreads) void attn_assign_kernel(AssignArgs 
         if (b < a.batch)
             base[b] = sat32(mine);
     }
+    behind = wave_sat_sum(behind);
+    if (l == 0)
+        behind_sums[wave] = behind;
     lds_barrier();
     const int bs = 1 << a.log2_bs;
     if ((int)blockIdx.x < a.token_workgroups) {
         if (blockIdx.x == 0 && tid == 0) {
             a.counts[0] = before < n_free ? (int)(n_free - before) : 0;
-            a.counts[1] = before > n_free ? sat32(before - n_free) : 0;
+            int64_t missing = before > n_free ? before - n_free : 0;
+            for (int w = 0; w < kAssignThreads / 64; ++w)
+                missing += behind_sums[w];
+            a.counts[1] = sat32(missing);
         }
 #pragma unroll 1
         for (int u = 0; u < kAssignTokens; ++u) {
@@ -306,7 +327,7 @@ hipError_t launch_attn_assign(int batch, int log2_bs, int max_blocks, int64_t T,
     const int64_t per = kAssignThreads * kAssignTokens;
     a.token_workgroups = (int)(T > 0 ? (T + per - 1) / per : 1);  // the first one also writes the counts
     a.table_workgroups = batch < 256 ? batch : 256;
-    const size_t lds = 2 * (size_t)batch * sizeof(int) + kAssignThreads / 64 * sizeof(int64_t);
+    const size_t lds = 2 * (size_t)batch * sizeof(int) + kAssignThreads / 64 * (sizeof(int64_t) + sizeof(uint32_t));
     hipLaunchKernelGGL(attn_assign_kernel, dim3((unsigned)(a.token_workgroups + a.table_workgroups)), dim3(kAssignThreads), lds,
                        stream, a);
     return hipGetLastError();

@@ -34,6 +34,64 @@ def test_assign_needs_beyond_32_bits(emu, tmp_path):
     assert len(set(given)) == len(given) and np.all(copies[:, :2] == -1)
 
 
+# Tables whose rows end in front of the last token: block size, width, new, cached, free blocks.
+NARROW = {
+    "some": (4, 2, [20], [2], 10),
+    "behind": (4, 2, [5], [11], 10),
+    "last_entry": (4, 2, [3, 1], [5, 8], 10),
+    "several": (8, 3, [1, 0, 30, 8, 5, 0, 17, 2], [0, 40, 7, 24, 23, 8, 30, 16], 40),
+    "and_short": (8, 3, [1, 0, 30, 8, 5, 0, 17, 2], [0, 40, 7, 24, 23, 8, 30, 16], 3),
+    "tokens": (1, 1, [3, 1, 4], [2, 0, 0], 20),
+    "many": (2, 2, [1 + i % 5 for i in range(300)], [i % 9 for i in range(300)], 350),
+}
+
+
+def narrow_problem(name):
+    """The call's arrays and what it has to say: entries behind the row's end take no block, and count as missing where new
+    tokens are theirs."""
+    bs, width, new, cached, n_free = NARROW[name]
+    batch = len(new)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    table = np.full((batch, width), -1, np.int32)
+    for b, c in enumerate(cached):
+        held = min(-(-c // bs), width)
+        table[b, :held] = b * width + np.arange(held)
+    free = 10000 + np.arange(n_free, dtype=np.int32)
+    shared = (np.arange(batch) % 3 != 1).astype(np.int32)
+    out, left, missing, slots, positions, copies = table.copy(), n_free, 0, [], [], []
+    for b, (n, c) in enumerate(zip(new, cached)):
+        copies.append([-1, -1, 0, 0])
+        for e in range(c // bs, -(-(c + n) // bs) if n else 0):
+            old = e < -(-c // bs)
+            if old and not shared[b] and e < width:
+                continue  # the last cached block takes more tokens
+            if e >= width or left == 0:
+                block, missing = -1, missing + 1
+            else:
+                left -= 1
+                block = int(free[left])
+            if e < width:
+                if old:
+                    copies[-1] = [int(table[b, e]), block, c % bs, 0]
+                out[b, e] = block
+        for p in range(c, c + n):
+            block = int(out[b, p // bs]) if p // bs < width else -1
+            slots.append(block * bs + p % bs if block >= 0 else -1)
+            positions.append(p)
+    want = (out, np.array(slots, np.int64), np.array(positions, np.int32), np.array(copies, np.int32), np.array([left, missing], np.int32))
+    return (bs, int(cu[-1]), cu, np.array(cached, np.int32), table, free, n_free, shared), want
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("name", sorted(NARROW))
+def test_assign_with_a_table_that_is_too_narrow(emu, tmp_path, name, in_place):
+    args, want = narrow_problem(name)
+    for order, side in ((0, "end"), (1, "start")):
+        got = _assign(emu, tmp_path, *args, in_place=in_place, order=order, side=side)
+        for g, w, what in zip(got, want, ("table", "slots", "positions", "copies", "counts")):
+            assert np.array_equal(g, w), f"{name}: {what}"
+
+
 # cu_seqlens, cached_lens; 40 tokens
 LENGTHS = {
     "decreasing": ([0, 30, 10, 40], [5, 0, 9]),
