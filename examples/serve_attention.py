@@ -99,7 +99,28 @@ class Server:
         """Serves (input, output) pairs as one batch.  Returns per request the tokens that were not computed and the rows of
         the last layer for all that were."""
         self.now += 1
-        looks = [self.cache.begin(inp, self.now) for inp, _ in requests]
+        looks = []
+        try:
+            for inp, _ in requests:
+                looks.append(self.cache.begin(inp, self.now))
+            lens, results, table, left = self._compute(requests, looks)
+        except BaseException:  # nothing is held yet: the hits' pins go back, the free list is as it was
+            for (inp, _), look in zip(requests, looks):
+                self.cache.abort(inp, look)
+            raise
+        del self.free[left:]
+        for (inp, out), look, row in zip(requests, looks, table):
+            full = inp + out
+            branch = self._hold(row[:-(-look.checkpoint_pos // self.block_size)]) if look.checkpoint_pos else None
+            final = self._hold(row[:-(-len(full) // self.block_size)])
+            evicted, rejected = self.cache.finish(full, look, branch, final, self.now)
+            for handle in evicted + rejected:
+                self._release(handle)
+        return lens, results
+
+    def _compute(self, requests, looks):
+        """The prefill and the tokens behind it.  Returns per request the tokens that were not computed and the rows of the others,
+        the table, and how many blocks are left of the free list."""
         table = torch.full((len(requests), self.width), -1, dtype=torch.int32)
         for b, look in enumerate(looks):
             if look.hit_len:
@@ -113,25 +134,18 @@ class Server:
         # a hit's last block may be read by other requests and be written to by the one that it belongs to
         step, rows = self._step(tokens, new, cached, table, pool, self._ints([len(self.free)]), self._ints([int(n > 0) for n in lens]))
         results = [[r] for r in rows.split(new)]
+        missing = step.counts[1:]  # of every step: a later one may need none
         for i in range(max(len(out) for _, out in requests)):
             cached = cached + self._ints(new)
             new = [int(i < len(out)) for _, out in requests]
             step, rows = self._step([out[i] for _, out in requests if i < len(out)], new, cached, table, pool, step.counts[:1])
+            missing = missing + step.counts[1:]
             for b, r in zip([b for b, n in enumerate(new) if n], rows.split(1)):
                 results[b].append(r)
-        left, missing = step.counts.tolist()
+        left, missing = torch.cat([step.counts[:1], missing]).tolist()
         if missing:
             raise RuntimeError(f"{missing} blocks missing: the cache's capacity leaves too few for a batch")
-        del self.free[left:]
-        table = table.tolist()
-        for (inp, out), look, row in zip(requests, looks, table):
-            full = inp + out
-            branch = self._hold(row[:-(-look.checkpoint_pos // self.block_size)]) if look.checkpoint_pos else None
-            final = self._hold(row[:-(-len(full) // self.block_size)])
-            evicted, rejected = self.cache.finish(full, look, branch, final, self.now)
-            for handle in evicted + rejected:
-                self._release(handle)
-        return lens, [torch.cat(r) for r in results]
+        return lens, [torch.cat(r) for r in results], table.tolist(), left
 
 
 def run(sessions=24, batch=8, window=0, sinks=0, dtype="bf16", n_layers=4, d_model=1024, n_q_heads=16, n_kv_heads=4, head_dim=64,

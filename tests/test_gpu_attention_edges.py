@@ -24,3 +24,11 @@ def test_assign_with_a_table_that_is_too_narrow(name, in_place):
                               shared_tail=_dev(shared), in_place=in_place)
     for g, w, what in zip(step, want, ("table", "slots", "positions", "copies", "counts")):
         assert np.array_equal(g.cpu().numpy(), w), f"{name}: {what}"
+
+
+def test_serving_without_enough_blocks_raises():
+    """The prefill of the first batch lacks blocks; the tokens behind it need none."""
+    from test_gpu_attention_example import _example
+    with pytest.raises(RuntimeError, match="missing"):
+        _example().run(sessions=4, batch=4, dtype="f32", n_layers=1, d_model=64, n_q_heads=1, n_kv_heads=1, n_blocks=3, block_size=64,
+                       prompt_len=(100, 101), user_len=(1, 2), out_len=(1, 2), capacity_bytes=1 << 20)
