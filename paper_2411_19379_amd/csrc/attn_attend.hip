@@ -11,6 +11,8 @@
 //
 // Rows that see only part of a tile of keys take their weights of the others as zero, and V's infinities and NaN in such
 // tiles stay out of the matrix product (0 * inf is not 0): they are added to the rows that see them one key at a time.
+#include <cfloat>
+
 #include "attn_common.h"
 
 #ifndef ATTN_TARGET  // workgroups that a launch is dealt to, where tests do not choose them
@@ -107,8 +109,6 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         o[db] = zero16();
     float m = -INFINITY, lsum = 0.f;
     bool seen = false;
-    const float outgrown = kOutgrown / a.scale_log2;
-
     // What this wave moves: KEYS neighbouring keys, of V of one tile and of K of the next; this lane piece load_at of its rows,
     // from where that piece of the row is.  With WIDE, blocks of at least KEYS keys, they lie in one block: one scalar look-up,
     // uniform addresses (32768 tokens over 16384 cached 16.4 ms against 18.6 with a look-up and an address per lane).  A key that does
@@ -288,7 +288,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 top = fmaxf(top, st[kb][r]);
-        if (__any(top > m + outgrown)) {
+        if (__any(top > m + a.outgrown)) {
             const float both = fmaxf(top, read_from(top, l ^ 32)), next = fmaxf(m, both);
             const float down = next == m ? 1.f : exp2_fast((m - next) * a.scale_log2);
             m = next;
@@ -607,7 +607,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
                     top = fmaxf(top, st[rb][kb][r]);
-            if (__any(top > m[rb] + kOutgrown / a.scale_log2)) {
+            if (__any(top > m[rb] + a.outgrown)) {
                 top = fmaxf(top, read_from(top, l ^ 16));
                 top = fmaxf(top, read_from(top, l ^ 32));
                 const float next = fmaxf(m[rb], top), down = next == m[rb] ? 1.f : exp2_fast((m[rb] - next) * a.scale_log2);
@@ -877,7 +877,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 top = fmaxf(top, st[kb][r]);
-        if (__any(top > m + kOutgrown / a.scale_log2)) {
+        if (__any(top > m + a.outgrown)) {
             top = fmaxf(top, read_from(top, l ^ 16));
             top = fmaxf(top, read_from(top, l ^ 32));
             const float next = fmaxf(m, top), down = next == m ? 1.f : exp2_fast((m - next) * a.scale_log2);
@@ -1258,6 +1258,8 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.window = window < kMostWindow ? window : kMostWindow;
     a.sinks = sinks;
     a.scale_log2 = scale * kLog2e;
+    // finite for the smallest scales as well: added to a maximum of minus infinity it stays minus infinity
+    a.outgrown = fminf(kOutgrown / a.scale_log2, FLT_MAX);
     a.part = static_cast<float *>(workspace);
     a.rows_cap = (int)u.rows_cap;
     a.most_parts = (int)u.parts;

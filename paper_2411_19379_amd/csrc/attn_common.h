@@ -99,6 +99,7 @@ struct AttendArgs {
     int32_t log2_bs, max_blocks, n_blocks;
     int32_t window, sinks;
     float scale_log2;       // scale * log2(e): the softmax runs on powers of two
+    float outgrown;         // by how much a score may exceed a row's maximum before the row is scaled down
     int32_t rows_cap;       // rows of a partial result
     int32_t most_parts;     // partial results there is room for
     uint32_t target;        // workgroups that keep the GPU busy

@@ -1,11 +1,12 @@
-"""Index arrays that no caller should pass: lengths that decrease, are negative or reach behind the arrays, sequences that name the
-same tokens, blocks and positions of nowhere.  Every buffer of the emulation lies against inaccessible pages, so an access
-outside the arguments ends the run; what the operators say of such a call has to make sense all the same."""
+"""Arguments at the edge of what the entry points take, and index arrays that no caller should pass: lengths that decrease, are
+negative or reach behind the arrays, sequences that name the same tokens, blocks and positions of nowhere.  Every buffer of the
+emulation lies against inaccessible pages, so an access outside the arguments ends the run; what the operators say of such a
+call has to make sense all the same."""
 import numpy as np
 import pytest
 
 import attn_helpers as ah
-from test_attention_emulation import _attend, _run, emu  # noqa: F401
+from test_attention_emulation import CASES, _attend, _run, emu  # noqa: F401
 
 MOST = 2 ** 31 - 1
 
@@ -164,3 +165,13 @@ def test_append_nowhere(emu, tmp_path):
         assert np.array_equal(got[2, 0, 3, 32:], qkv[6].reshape(-1, d)[part, 32:]) and np.array_equal(got[0, 0, 0, 32:], qkv[8].reshape(-1, d)[part, 32:])
     q = flat[:T * hq * d].reshape(T, hq, d)
     assert np.isnan(q[:4, :, :32]).all() and np.isfinite(q[4:]).all()
+
+
+@pytest.mark.parametrize("scale", [8.3e-39, 1.3e-38, 2.3e-38, 2.4e-38])
+@pytest.mark.parametrize("name", ["decode", "few_tokens_wide", "chunk", "f32"])
+def test_attend_smallest_scales(emu, tmp_path, name, scale):
+    """From the smallest scale that is accepted on: every key weighs the same, and lse is the log of their number."""
+    p = ah.make(11, *CASES[name])
+    p.scale = float(np.float32(scale))
+    for target in (2, 30):
+        ah.check(p, *_attend(emu, tmp_path, p, target=target), f"{name} {scale}")

@@ -3,7 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+import attn_helpers as ah
+from test_attention_emulation import CASES
 from test_attention_malformed import NARROW, narrow_problem
+from test_gpu_attention import _attend
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -32,3 +35,12 @@ def test_serving_without_enough_blocks_raises():
     with pytest.raises(RuntimeError, match="missing"):
         _example().run(sessions=4, batch=4, dtype="f32", n_layers=1, d_model=64, n_q_heads=1, n_kv_heads=1, n_blocks=3, block_size=64,
                        prompt_len=(100, 101), user_len=(1, 2), out_len=(1, 2), capacity_bytes=1 << 20)
+
+
+@pytest.mark.parametrize("scale", [8.3e-39, 1.3e-38, 2.4e-38])
+@pytest.mark.parametrize("name", ["decode", "few_tokens_wide", "chunk", "f32"])
+def test_attend_smallest_scales(name, scale):
+    print(f"attend scale {name} {scale}", flush=True)
+    p = ah.make(11, *CASES[name])
+    p.scale = float(np.float32(scale))
+    ah.check(p, *_attend(p), f"{name} {scale}")
