@@ -166,7 +166,8 @@ int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total
  *
  *     out = sum_j softmax_j(scale * q . k_j) v_j,    lse = ln sum_j exp(scale * q . k_j)
  *
- * over the keys it sees; a query that sees none gets out = 0, lse = -inf.
+ * over the keys it sees; a query that sees none gets out = 0, lse = -inf.  One
+ * whose largest scaled score is minus infinity or beyond fp32 gets NaN.
  * Statistics and sums are fp32; with 16-bit types the weights are rounded to
  * the type for the product with v.
  *

@@ -364,7 +364,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         return;
     lsum += read_from(lsum, l ^ 32);
     const int seen_there = read_from((int)seen, l ^ 32);
-    const float w = row_weight(lsum, m, seen || seen_there != 0);
+    const float w = row_weight(lsum, seen || seen_there != 0);
     const bool split = it.n_splits > 1;
     const int part = split ? part_of(a, it, kv_head, it.split) : 0;
     if (split && part >= a.most_parts)
@@ -680,7 +680,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
             *reinterpret_cast<float4 *>(lds_o + (wave * 16 + l % 16) * (D + 4) + db * 16 + 4 * quarter) =
                 make_float4(o[rb][db][0], o[rb][db][1], o[rb][db][2], o[rb][db][3]);
         if (quarter == 0)
-            *reinterpret_cast<float2 *>(lds_ml + (wave * 16 + l) * 2) = make_float2(m[rb], row_weight(w, m[rb], any != 0));
+            *reinterpret_cast<float2 *>(lds_ml + (wave * 16 + l) * 2) = make_float2(m[rb], row_weight(w, any != 0));
         lds_barrier();
         // thread: row tid / 16, values 4 (tid % 16) and every 64 behind them
         const int row = tid / 16, full_row = r0 + 16 * rb + row;
@@ -938,7 +938,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
     int any = (int)seen;
     any |= read_from(any, l ^ 16);
     any |= read_from(any, l ^ 32);
-    const float w = row_weight(lsum, m, any != 0);
+    const float w = row_weight(lsum, any != 0);
     if (!row_works)
         return;
     const bool split = it.n_splits > 1;

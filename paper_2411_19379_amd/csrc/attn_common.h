@@ -372,9 +372,9 @@ __device__ __forceinline__ float not_finite_part(float p, float v, uint32_t sees
 // Weight of a row's maximum: 0 where nothing finite has been seen yet, so that no infinity is subtracted from itself.
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-// How a row without any weight is marked in a partial result: it saw no key (0), or only scores of minus infinity (-1), of
-// which the softmax is undefined.
-__device__ __forceinline__ float row_weight(float l, float m, bool seen) { return m == -INFINITY && l == 0.f && seen ? -1.f : l; }
+// How a row without any weight is marked in a partial result: it saw no key (0), or only scores of minus infinity or beyond fp32,
+// of which the softmax is undefined (-1).
+__device__ __forceinline__ float row_weight(float l, bool seen) { return l == 0.f && seen ? -1.f : l; }
 
 // ln of the sum of exponentials of a row whose weights are powers of two of scale_log2 (score - m).
 __device__ __forceinline__ float row_lse(float m, float w, float scale_log2)
@@ -387,7 +387,7 @@ __device__ __forceinline__ float row_lse(float m, float w, float scale_log2)
 // A row put together from partial results (maximum, weight): first every maximum, then every weight.
 struct JoinedRow {
     float m = -INFINITY, w = 0.f;
-    bool undefined = false;  // a part saw only scores of minus infinity
+    bool undefined = false;  // a part saw keys and has no weight
     __device__ __forceinline__ void add_max(float part_m) { m = fmaxf(m, part_m); }
     // the factor of the part's sums; 0 if the part has none
     __device__ __forceinline__ float add_weight(float part_m, float part_w, float scale_log2)

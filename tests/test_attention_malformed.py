@@ -175,3 +175,22 @@ def test_attend_smallest_scales(emu, tmp_path, name, scale):
     p.scale = float(np.float32(scale))
     for target in (2, 30):
         ah.check(p, *_attend(emu, tmp_path, p, target=target), f"{name} {scale}")
+
+
+@pytest.mark.parametrize("name", ["decode", "few_tokens_wide", "chunk_group", "f32"])
+def test_attend_scores_beyond_fp32(emu, tmp_path, name):
+    """A row whose largest scaled score has no place in fp32 says so: NaN, not the zeros of a row that sees nothing."""
+    p = ah.make(11, *CASES[name])
+    p.scale = 1e38
+    top = np.full((p.T, p.hq), np.nan)
+    for b, (n, c) in enumerate(zip(p.new, p.cached)):
+        for i in range(n):
+            rows = [p.block_row(b, j) for j in range(c + i + 1)]
+            for h in range(p.hq):
+                k = np.stack([p.k_cache[block, h // (p.hq // p.hkv), r].double().numpy() for block, r in rows])
+                top[p.cu[b] + i, h] = (k @ p.q[p.cu[b] + i, h].double().numpy()).max()
+    beyond = np.abs(top) > 4.0  # 4e38 is behind fp32's end
+    assert beyond.sum() > 0.5 * beyond.size
+    for target in (2, 30):
+        out, lse = _attend(emu, tmp_path, p, target=target)
+        assert np.isnan(out[beyond]).all() and np.isnan(lse[beyond]).all(), f"{name} {target}"

@@ -44,3 +44,13 @@ def test_attend_smallest_scales(name, scale):
     p = ah.make(11, *CASES[name])
     p.scale = float(np.float32(scale))
     ah.check(p, *_attend(p), f"{name} {scale}")
+
+
+@pytest.mark.parametrize("name", ["decode", "few_tokens_wide", "chunk_group", "f32"])
+def test_attend_scores_beyond_fp32(name):
+    """Rows whose scaled scores fp32 has no place for are NaN; none looks like a row that sees nothing."""
+    print(f"attend beyond fp32 {name}", flush=True)
+    p = ah.make(11, *CASES[name])
+    p.scale = 1e38
+    out, lse = _attend(p)
+    assert not np.any(np.isneginf(lse)) and np.isnan(out).all(-1).mean() > 0.5
