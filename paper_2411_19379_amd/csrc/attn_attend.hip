@@ -1,8 +1,10 @@
 // Attention of the new tokens of a packed batch over the paged cache: for chunks of prompts, for single tokens, and in fp32.
 //
 // One pass over the keys with a running maximum m and weight l per row:  p = 2^(c (s - m)),  l = sum p,  O = sum p v,  with
-// c = scale log2(e); when a row's scores outgrow m, what has been summed is scaled down.  A query head reads the key head of
-// its group, so the rows of a sequence are (token, head of the group) pairs: all that read one key head.
+// c = scale log2(e); when a row's scores outgrow m, what has been summed is scaled down.  With 16-bit types p is rounded to the type
+// for the product with v, since the matrix instructions take no other, and l is the sum of what has not been rounded; all sums
+// are fp32.  A query head reads the key head of its group, so the rows of a sequence are (token, head of the group) pairs: all
+// that read one key head.
 //
 // All three kernels compute S^T = K Q^T, keys down the matrix rows, so that a lane holds scores of one row of the problem and
 // keeps that row's m and l in registers, and O^T = V^T P^T, of which the lane's accumulators are the same row again.  The
@@ -21,7 +23,7 @@
 
 namespace {
 
-constexpr float kOutgrown = 8.f;  // powers of two by which a weight may exceed 1 before its row is scaled down
+constexpr float kOutgrown = 8.f;  // powers of two by which a weight may exceed that of the maximum before its row is scaled down
 
 template <typename E> __device__ __forceinline__ void unpack4(uint2 u, float *v)
 {
@@ -299,7 +301,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
                 for (int r = 0; r < 16; ++r)
                     o[db][r] *= down;
         }
-        const float mc = finite_max(m) * a.scale_log2;
+        const float mc = subtrahend<E>(m, a.scale_log2);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             float p[16];
@@ -374,7 +376,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         if (split)
             *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + (part_row + l % 32) * 2) = make_float2(m, w);
         else if (a.lse)
-            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
+            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse<E>(m, w, a.scale_log2);
     }
     // A lane holds values of one row all over the head: through LDS, half of the head at a time, to rows that leave in whole lines.
     constexpr int COLS = D / 2, STRIDE = COLS + 4, LANES = COLS / 4, ROWS_AT_ONCE = 64 / LANES;
@@ -619,7 +621,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
                     for (int r = 0; r < 4; ++r)
                         o[rb][db][r] *= down;
             }
-            const float mc = finite_max(m[rb]) * a.scale_log2;
+            const float mc = subtrahend<E>(m[rb], a.scale_log2);
             float p[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -718,7 +720,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
                     if (it.n_splits > 1)
                         *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(j.m, j.weight());
                     else if (a.lse)
-                        a.lse[(int64_t)(s.start + tok) * a.Hq + hd] = row_lse(j.m, j.weight(), a.scale_log2);
+                        a.lse[(int64_t)(s.start + tok) * a.Hq + hd] = row_lse<E>(j.m, j.weight(), a.scale_log2);
                 }
             }
         }
@@ -889,7 +891,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
                 for (int r = 0; r < 4; ++r)
                     o[db][r] *= down;
         }
-        const float mc = finite_max(m) * a.scale_log2;
+        const float mc = subtrahend<float>(m, a.scale_log2);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float p = exp2_fast(__builtin_fmaf(st[e / 4][e % 4], a.scale_log2, -mc));
@@ -956,7 +958,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         if (split)
             *reinterpret_cast<float2 *>(a.part + (int64_t)a.most_parts * a.rows_cap * D + at * 2) = make_float2(m, w);
         else if (a.lse)
-            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(m, w, a.scale_log2);
+            a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse<float>(m, w, a.scale_log2);
     }
 }
 
@@ -1048,7 +1050,7 @@ template <typename E, int D, int ROWS> __device__ __forceinline__ void join_row(
     if (l < LANES)
         Out<E>::store4(a.out, (int64_t)(s.start + token) * a.out_stride + (int64_t)head * D + 4 * l, v);
     if (a.lse && l == 0)
-        a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse(j.m, j.weight(), a.scale_log2);
+        a.lse[(int64_t)(s.start + token) * a.Hq + head] = row_lse<E>(j.m, j.weight(), a.scale_log2);
 }
 
 // `rows` rows at a time, `blocks` times per (tile, key head); the workgroups of the launch take them in turn until there are

@@ -333,6 +333,7 @@ __device__ __forceinline__ int cache_row(const AttendArgs &a, int block, int kv_
 // ---------------------------------------------------------------- 16-bit types
 struct Bf16 {
     static constexpr uint32_t kExp = 0x7f80u;
+    static constexpr float kPowers = 0.f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack2_bf16(lo, hi); }
     static __device__ __forceinline__ float lo(uint32_t u) { return bf16_lo(u); }
     static __device__ __forceinline__ float hi(uint32_t u) { return bf16_hi(u); }
@@ -344,6 +345,7 @@ struct Bf16 {
 };
 struct F16 {
     static constexpr uint32_t kExp = 0x7c00u;
+    static constexpr float kPowers = 7.f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack2_f16(lo, hi); }
     static __device__ __forceinline__ float lo(uint32_t u) { return f16_lo(u); }
     static __device__ __forceinline__ float hi(uint32_t u) { return f16_hi(u); }
@@ -369,19 +371,35 @@ __device__ __forceinline__ float not_finite_part(float p, float v, uint32_t sees
     return __uint_as_float(__float_as_uint(p * v) & is & sees);
 }
 
-// Weight of a row's maximum: 0 where nothing finite has been seen yet, so that no infinity is subtracted from itself.
+// Weights are 2^(scale_log2 (score - m) + powers of the type).  The product with v takes them rounded to 16 bits, the sum of weights
+// as they are.  In fp16 a weight below 2^-25 is nothing to the product, but counts in the sum: so the largest of a row is 2^7 (and
+// 2^15 where m lags behind, which fp16 still holds), and keys count down to 2^-32 of it (behind a key of weight 1 and value 0, 1500
+// of 2^-24 to 2^-28 came out as three quarters of their sum).
+template <typename E> struct Weights {
+    static constexpr float kPowers = E::kPowers;
+};
+template <> struct Weights<float> {
+    static constexpr float kPowers = 0.f;
+};
+// What is subtracted from a row's scaled scores.  The maximum is taken as 0 where nothing finite has been seen yet, so that no
+// infinity is subtracted from itself.
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
+template <typename E> __device__ __forceinline__ float subtrahend(float m, float scale_log2)
+{
+    constexpr float powers = Weights<E>::kPowers;
+    return powers == 0.f ? finite_max(m) * scale_log2 : __builtin_fmaf(finite_max(m), scale_log2, -powers);
+}
 
 // How a row without any weight is marked in a partial result: it saw no key (0), or only scores of minus infinity or beyond fp32,
 // of which the softmax is undefined (-1).
 __device__ __forceinline__ float row_weight(float l, bool seen) { return l == 0.f && seen ? -1.f : l; }
 
-// ln of the sum of exponentials of a row whose weights are powers of two of scale_log2 (score - m).
-__device__ __forceinline__ float row_lse(float m, float w, float scale_log2)
+// ln of the sum of exponentials of a row with this maximum and sum of weights.
+template <typename E> __device__ __forceinline__ float row_lse(float m, float w, float scale_log2)
 {
     if (w == 0.f)
         return -INFINITY;
-    return w < 0.f ? NAN : (m * scale_log2 + __builtin_amdgcn_logf(w)) * 0.69314718055994531f;
+    return w < 0.f ? NAN : (m * scale_log2 + (__builtin_amdgcn_logf(w) - Weights<E>::kPowers)) * 0.69314718055994531f;
 }
 
 // A row put together from partial results (maximum, weight): first every maximum, then every weight.

@@ -4,6 +4,7 @@ emulation lies against inaccessible pages, so an access outside the arguments en
 call has to make sense all the same."""
 import numpy as np
 import pytest
+import torch
 
 import attn_helpers as ah
 from test_attention_emulation import CASES, _attend, _run, emu  # noqa: F401
@@ -194,3 +195,37 @@ def test_attend_scores_beyond_fp32(emu, tmp_path, name):
     for target in (2, 30):
         out, lse = _attend(emu, tmp_path, p, target=target)
         assert np.isnan(out[beyond]).all() and np.isnan(lse[beyond]).all(), f"{name} {target}"
+
+
+def light_weights(max_new, dtype="f16", keys=1500, new=1):
+    """One key in front outweighs each of the others by 2^24 to 2^28; its value is 0, theirs are around 1000."""
+    p = ah.make(29, 2, 1, 64, 16, dtype, [new], [keys], max_new=max_new)
+    g = torch.Generator().manual_seed(4)
+    p.q[:] = 0
+    p.q[:, :, 0] = 8.0
+    for j in range(keys + new):
+        block, row = p.block_row(0, j)
+        p.k_cache[block, 0, row] = 0
+        p.k_cache[block, 0, row, 0] = 18.0 if j == 0 else float(torch.rand(1, generator=g)) * 2.8 - 1.4
+        p.v_cache[block, 0, row] = 0 if j == 0 else (1000 + 50 * torch.randn(64, generator=g)).to(p.v_cache.dtype)
+    return p
+
+
+def check_light_weights(p, out, lse, what):
+    """A weight of fp16 is off by half an ulp or, below the smallest normal number, by 2^-25; the largest of a row is 2^7 at least.
+    The result is rounded once, and its own subnormal numbers are 2^-24 apart."""
+    want, want_lse, size = ah.reference(p)
+    u = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[p.dtype]
+    tol = (2 * u + 1e-5) * size + ((p.new[0] + p.cached[0]) * 1200 * 2.0 ** -32 + 2.0 ** -25 if p.dtype == "f16" else 0)
+    assert np.all(tol < 0.1 * np.abs(want))  # a row without them is far out
+    assert np.abs(out - want).max() <= tol.max() and np.all(np.abs(out - want) <= tol), f"{what}: {(np.abs(out - want) / tol).max():.1f} times the bound"
+    assert np.all(np.abs(lse - want_lse) <= 1e-5 * (1 + np.abs(want_lse)))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("max_new,new", [(1, 1), (0, 40)])
+def test_attend_many_light_keys(emu, tmp_path, max_new, new, dtype):
+    """Weights far below a row's largest one count, in the sum with v as in the sum of weights."""
+    p = light_weights(max_new, dtype, new=new)
+    for target in (1, 20):
+        check_light_weights(p, *_attend(emu, tmp_path, p, target=target), f"{new} {target}")

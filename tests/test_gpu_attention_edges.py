@@ -5,7 +5,7 @@ import torch
 
 import attn_helpers as ah
 from test_attention_emulation import CASES
-from test_attention_malformed import NARROW, narrow_problem
+from test_attention_malformed import NARROW, check_light_weights, light_weights, narrow_problem
 from test_gpu_attention import _attend
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +54,11 @@ def test_attend_scores_beyond_fp32(name):
     p.scale = 1e38
     out, lse = _attend(p)
     assert not np.any(np.isneginf(lse)) and np.isnan(out).all(-1).mean() > 0.5
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("max_new,new", [(1, 1), (0, 40)])
+def test_attend_many_light_keys(max_new, new, dtype):
+    print(f"attend light keys {dtype} {new}", flush=True)
+    p = light_weights(max_new, dtype, new=new)
+    check_light_weights(p, *_attend(p), f"{dtype} {new}")
