@@ -29,17 +29,28 @@ __device__ __forceinline__ uint32_t lds_address(const void *p)
 {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void *)p;
 }
+// The copies below write M0.  In front of a copy and behind it this tells the compiler, so that nothing that it keeps there lives
+// across one: a value in M0 that a use in front needs stays in front, and a use behind gets its own.
+__device__ __forceinline__ void m0_is_lost()
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    __asm__ volatile("" ::: "m0", "memory");
+#endif
+}
 // 16 bytes per lane from memory right into LDS: lane l's, `offset` bytes behind `from`, go to `to` + 16 l; `from` and `to` are
-// the same for the whole wave.  They are there after the wave's next memory_wait(); the wave must wait before it ends.  (M0
-// holds nothing else in these kernels: there is no other use of it in what is compiled.)
+// the same for the whole wave.  They are there after the wave's next memory_wait(); the wave must wait before it ends.
 __device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t offset, uint32_t to)
 {
+    m0_is_lost();
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(from), "s"(to) : "memory");
+    m0_is_lost();
 }
 // The same with an address per lane.
 __device__ __forceinline__ void copy16_to_lds(const void *from, uint32_t to)
 {
+    m0_is_lost();
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+    m0_is_lost();
 }
 __device__ __forceinline__ void memory_wait() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
