@@ -5,7 +5,8 @@
     out = attend(q, k_cache, v_cache, step.table, cu_seqlens, cached_lens)
 
 All of it is enqueued on the current torch stream, nothing waits for the GPU, and lengths are read there; outputs and the
-workspace are torch tensors.  There is no CPU fallback: loading raises if the library has not been built.
+workspace are torch tensors.  There is no CPU fallback: loading raises if the library has not been built.  There is no backward
+pass either: where a graph is recorded, tensors that require grad are refused (serve under `torch.no_grad()`).
 """
 from __future__ import annotations
 

@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -82,6 +83,19 @@ void *rows(const char *name, const at::Tensor &t, std::initializer_list<int64_t>
                       ": the heads of a token must be contiguous, got strides ", t.strides());
     *stride = tokens > 1 ? t.stride(0) : heads * dim;
     return t.data_ptr();
+}
+
+// There is no backward pass: where a graph is recorded, a result outside it would drop gradients in silence.
+struct Named {
+    const char *name;
+    const at::Tensor *t;
+};
+void no_gradients(std::initializer_list<Named> all)
+{
+    if (!c10::GradMode::is_enabled())
+        return;
+    for (const Named &n : all)
+        TORCH_CHECK_VALUE(!n.t->requires_grad(), n.name, " requires grad, and this operator has no backward pass: call it under torch.no_grad(), or detach");
 }
 
 int on_current_device(const at::Tensor &t)
@@ -183,6 +197,11 @@ PyObject *rope_append(PyObject *, PyObject *const *args, Py_ssize_t n)
     arguments(n, 11);
     const at::Tensor &q = tensor(args[0], "q"), &k = tensor(args[1], "k"), &v = tensor(args[2], "v"), &slots = tensor(args[4], "slots"),
                      &k_cache = tensor(args[6], "k_cache"), &v_cache = tensor(args[7], "v_cache");
+    no_gradients({{"q", &q}, {"k", &k}, {"v", &v}, {"k_cache", &k_cache}, {"v_cache", &v_cache}});
+    if (args[5] != Py_None)
+        no_gradients({{"rotary", &tensor(args[5], "rotary")}});
+    if (args[10] != Py_None)
+        no_gradients({{"q_out", &tensor(args[10], "q_out")}});
     const int device = on_current_device(q);
     const at::ScalarType type = q.scalar_type();
     void *k_to, *v_to;
@@ -226,6 +245,9 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n)
     arguments(n, 12);
     const at::Tensor &q = tensor(args[0], "q"), &k_cache = tensor(args[1], "k_cache"), &v_cache = tensor(args[2], "v_cache"), &table = tensor(args[3], "table"),
                      &cu = tensor(args[4], "cu_seqlens"), &cached = tensor(args[5], "cached_lens");
+    no_gradients({{"q", &q}, {"k_cache", &k_cache}, {"v_cache", &v_cache}});
+    if (args[10] != Py_None)
+        no_gradients({{"out", &tensor(args[10], "out")}});
     const int device = on_current_device(q);
     const at::ScalarType type = q.scalar_type();
     void *k_at, *v_at;
