@@ -98,6 +98,13 @@ void no_gradients(std::initializer_list<Named> all)
         TORCH_CHECK_VALUE(!n.t->requires_grad(), n.name, " requires grad, and this operator has no backward pass: call it under torch.no_grad(), or detach");
 }
 
+// A tensor of the caller's has been written: what autograd keeps of it is out of date.  (Inference tensors have no version.)
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference())
+        t.unsafeGetTensorImpl()->bump_version();
+}
+
 int on_current_device(const at::Tensor &t)
 {
     TORCH_CHECK_VALUE(t.is_cuda() && t.get_device() == c10::hip::current_device(), "expected tensors on the current CUDA device, got ", t.device());
@@ -180,6 +187,8 @@ PyObject *assign_blocks(PyObject *, PyObject *const *args, Py_ssize_t n)
                              static_cast<int32_t *>(out.data_ptr()), free_at, n_free_at, size32(free_blocks.numel(), "free_blocks"),
                              static_cast<int64_t *>(slots.data_ptr()), static_cast<int32_t *>(positions.data_ptr()),
                              static_cast<int32_t *>(copies.data_ptr()), static_cast<int32_t *>(counts.data_ptr()), stream(device)));
+    if (in_place)
+        written(table);
     PyObject *r = PyTuple_New(5);
     if (!r)
         throw python_error();
@@ -234,6 +243,10 @@ PyObject *rope_append(PyObject *, PyObject *const *args, Py_ssize_t n)
     void *out_at = address("q_out", out, {T, s.n_q_heads, s.head_dim}, type, device);
     check(attn_rope_append(&s, T, batch, size32(k_cache.size(0), "n_blocks"), q_at, q_stride, k_at, k_stride, v_at, v_stride, positions_at, slots_at,
                            rotary_at, most, dim, interleaved, copies_at, out_at, k_to, v_to, stream(device)));
+    written(k_cache);
+    written(v_cache);
+    if (args[10] != Py_None)
+        written(out);
     return THPVariable_Wrap(out);
     END_HANDLE_TH_ERRORS
 }
@@ -277,6 +290,8 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n)
     check(attn_attend(&s, (int32_t)batch, T, size32(k_cache.size(0), "n_blocks"), size32(table.size(1), "the table's width"), q_at, q_stride, k_at, v_at,
                       table_at, cu_at, cached_at, scale, window, sinks, max_new, out_at, out_stride, want_lse ? static_cast<float *>(lse.data_ptr()) : nullptr,
                       need ? workspace.data_ptr() : nullptr, need, stream(device)));
+    if (args[10] != Py_None)
+        written(out);
     if (!want_lse)
         return THPVariable_Wrap(out);
     PyObject *r = PyTuple_New(2);

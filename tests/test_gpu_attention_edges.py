@@ -62,3 +62,31 @@ def test_attend_many_light_keys(max_new, new, dtype):
     print(f"attend light keys {dtype} {new}", flush=True)
     p = light_weights(max_new, dtype, new=new)
     check_light_weights(p, *_attend(p), f"{dtype} {new}")
+
+
+def test_what_is_written_gets_a_new_version():
+    """Autograd keeps a cache (or `out`, q_out, a table) for a backward pass: written since, it is refused there as any tensor
+    that was changed in place; what the calls only read stays as it is."""
+    from paper_2411_19379_amd import attention as attn
+    h = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device=DEV)
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device=DEV)
+    table, free, n_free, cu, lens = z(1, 4), torch.arange(5, dtype=torch.int32, device=DEV), z(1) + 5, torch.tensor([0, 3], dtype=torch.int32, device=DEV), z(1)
+    k_cache, v_cache, q, k = h(5, 2, 16, 64), h(5, 2, 16, 64), h(3, 4, 64), h(3, 2, 64)
+    q_out, out = h(3, 4, 64), h(3, 4, 64)
+    read = [free, n_free, cu, lens, q, k]
+    w = torch.ones((), dtype=torch.bfloat16, device=DEV, requires_grad=True)
+    losses = [(x * w).sum() for x in (k_cache, v_cache, q_out, out)]
+    before, read_before = [x._version for x in (table, k_cache, v_cache, q_out, out)], [x._version for x in read]
+    step = attn.assign_blocks(16, 3, cu, lens, table, free, n_free, in_place=True)
+    attn.rope_append(q, k, k, step.positions, step.slots, None, k_cache, v_cache, q_out=q_out)
+    attn.attend(q_out, k_cache, v_cache, step.table, cu, lens, out=out)
+    assert all(x._version > b for x, b in zip((table, k_cache, v_cache, q_out, out), before))
+    assert [x._version for x in read] == read_before
+    for loss in losses:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    with torch.inference_mode():  # tensors without versions
+        caches = h(5, 2, 16, 64), h(5, 2, 16, 64)
+        made = h(3, 4, 64)
+        attn.rope_append(q, k, k, step.positions, step.slots, None, *caches, q_out=made)
+    attn.attend(made, *caches, step.table, cu, lens, out=made)
