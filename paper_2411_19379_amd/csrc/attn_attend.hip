@@ -43,9 +43,13 @@ template <typename E> __device__ __forceinline__ void unpack4(uint2 u, float *v)
 // of its products t + 1, phase 2t + 2 or 2t + 3, and the first reads are in phase 2t + 4.
 //
 // With 128 values per head a tile of a wave is 1024 cycles of products and about 870 of softmax: the matrix cores bind, at the
-// clock that the power allows (32768 tokens over 16384 cached, 32 heads, bf16: 15.0 ms, 1170 TFLOP/s, matrix cores busy 62 % of
-// the cycles at 1.8 GHz).  With 64 the products are half as many and the softmax the same, which binds (16 packed prompts of 512
-// to 4096 tokens, 16 heads, fp16: 316 us, 620 TFLOP/s).  A tile of 256 rows by 64 keys needs 32 KB from the L2 for some 2 us.
+// clock that the power allows (32768 tokens over 16384 cached, 32 heads, bf16: 15.1 ms, 1160 TFLOP/s, matrix cores busy 62 % of
+// the cycles at 1.8 GHz; a library's product of 16384 reaches 1580).  With 64 the products are half as many and the softmax the
+// same, which binds: 188 vector instructions per tile and wave, those around the loop included, beside 16 matrix instructions (16
+// packed prompts of 512 to 4096 tokens, 16 heads, fp16: 312 us, 630 TFLOP/s).  There the pieces also go out sequence by sequence,
+// which by their steps ends 27 % behind an even spread over the 512 workgroups that are resident, and 9 registers (14 with blocks of
+// fewer than 8 tokens) go to memory at the 128 that four waves of a SIMD leave each other.  A tile of 256 rows by 64 keys needs
+// 32 KB from the L2 for some 2 us.
 constexpr int kChunkKeys = 64;
 
 constexpr int kChunkBuffers = 3;
@@ -415,8 +419,9 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
 // For the rows of single tokens, 16 RB of them at a time: each of the four waves takes every fourth tile of 32 keys, K from
 // memory right into the operand's registers, V through LDS of its own for the transposing reads; no barriers until the waves'
 // results are joined.  What bounds it is reading the cache, once: a wave's next tile is requested before the present one is used
-// (64 requests over 512 to 8192 keys, 8 key heads of 128, bf16: 136 us, 5.1 TB/s; 256 with a window of 1024: 149 us, 5.1 TB/s, the
-// rate of a large copy).  A single request over 4012 keys is latency: 14 us, 8 of them this kernel and 5 the join.
+// (64 requests over 512 to 8192 keys, 8 key heads of 128, bf16: 129 us, 5.4 TB/s; 256 with a window of 1024: 147 us, 5.2 TB/s; a
+// large copy reaches 5.4, a sweep in place 6.0).  A single request over 4012 keys is latency: a call of 14 us, 8 to 10 of them
+// this kernel and 5 the join.
 constexpr int kFewKeys = 32;
 constexpr int kFewWaves = 4;
 
@@ -731,8 +736,9 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
 // ================================================================ fp32
 // 16 rows per wave, 64 per workgroup, keys in tiles of 32 through LDS in two buffers; products on the fp32 matrix instructions,
 // which take 2048 cycles of a wave's 4000 to 5100 per tile with heads of 64 (a sixteenth of the 16-bit rate): 3 packed prompts of
-// 1537 tokens with a window of 300, 16 heads of 64, 38 us, 48 TFLOP/s; a prompt of 2000 tokens 126 us, 65 TFLOP/s.  Keys from
-// two tiles ahead, in registers, and addresses from scalar look-ups changed nothing.
+// 1537 tokens with a window of 300, 16 heads of 64, 38 us, 47 TFLOP/s; a prompt of 2000 tokens 127 us, 65 TFLOP/s.  The former is
+// 392 workgroups on 256 compute units: half of them have two, and end last.  Keys from two tiles ahead, in registers, and
+// addresses from scalar look-ups changed nothing.  For single tokens one of the four waves has rows.
 constexpr int kF32Keys = 32;
 constexpr int kF32Waves = 4;
 
@@ -1105,7 +1111,9 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32
     c.parts = 2 * (int64_t)c.target;
     c.rows_cap = rows < all_rows ? rows : all_rows;
     const int64_t split_tiles = c.most_tiles * s.n_kv_heads < c.target ? c.most_tiles * s.n_kv_heads : c.target;
-    c.join_rows = c.rows_cap <= 16 ? 4 : 8;   // few rows: all at once; many: fewer look-ups of who they are
+    // few rows: all at once (32 requests of one token with a single key head 32 us, eight by eight 38); many: fewer look-ups of who
+    // they are (2 requests of 100 and 300 tokens 41 us, four by four 44; but the chat turn 32, 31)
+    c.join_rows = c.rows_cap <= 16 ? 4 : 8;
     c.join_blocks = (c.rows_cap + c.join_rows - 1) / c.join_rows;
     c.join_units = (split_tiles + s.n_kv_heads - 1) / s.n_kv_heads * s.n_kv_heads * c.join_blocks;
     c.join_grid = c.join_units < kJoinWorkgroups ? c.join_units : kJoinWorkgroups;
@@ -1122,6 +1130,12 @@ Launch make_launch(const attn_shape_t &s, int batch, int64_t T, int rows, uint32
 // some sequences of a batch and the one for few rows for the others, a launch and a join each, lost nearly everywhere: 5
 // requests of 20 to 60 tokens 30.7 us against 25.9, 64 of 1 to 512 tokens 540 against 489, of 1 to 24 221 against 226.)  Without
 // a hint a batch with no more tokens than sequences is taken for single tokens.
+//
+// Up to 32 rows the kernel for few rows was no slower in any batch measured, and the limit is not the crossing.  With heads of 128 (one request
+// over 4000 keys / 64 over up to 4000; few rows against chunks): 32 rows 21 / 97 us against 21 / 171, 48 rows 27 / 139 against 21 /
+// 173, 96 rows 30 / 190 against 22 / 179.  With heads of 64 it lies behind 96 rows: 17 / 91 us against 19 / 133.  Two blocks
+// of 16 rows read the keys of 17 to 32 rows once, two tiles of 16 twice: 64 requests of 32 rows 97 us against 104, but 16 such
+// requests 49 against 41, one 21 against 16.  Up to 16 rows one block is never slower (one request 13, two blocks 17).
 Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
 {
     Choice c;
@@ -1138,7 +1152,8 @@ Choice choose(const attn_shape_t &s, int batch, int64_t T, int max_new)
     } else {
         c.chunk = true;
         // Partial results of less than a tile's rows cost little: 32 requests of 16 tokens with 64 rows of heads 116 us, shared by 256
-        // workgroups 172.  Those of whole tiles cost more than the balance gives: 4 prompts of 500 to 1500 tokens 48, 45.
+        // workgroups 172 (16 of 56 tokens 80, 72).  Those of whole tiles cost more than the balance gives: a prompt of 2000 tokens
+        // 88 us shared by 512, 61 by 256, 4 of 500 to 1500 tokens 49, 46 (16 of 80 to 128 tokens 98 to 123, 136 to 140).
         c.launch = rows < kChunkRows ? make_launch(s, batch, T, kChunkRows, 512, 6, 16) : make_launch(s, batch, T, kChunkRows, 256, 6, 0);
     }
     return c;

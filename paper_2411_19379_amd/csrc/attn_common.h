@@ -322,6 +322,8 @@ template <int PER, int ROWS, int KT> __device__ __forceinline__ bool find_among(
     }
     return false;
 }
+// A sequence per lane as long as that reaches: 64 requests of one token 73 us, four per lane 77; 65 to 128 requests the same either
+// way, 256 with four per lane 214, with one 218.
 template <int ROWS, int KT> __device__ __forceinline__ bool find_item(const AttendArgs &a, int unit, bool of_join, Item *out)
 {
     return a.batch <= 64 ? find_among<1, ROWS, KT>(a, unit, of_join, out) : find_among<4, ROWS, KT>(a, unit, of_join, out);
