@@ -4,6 +4,14 @@
     q = rope_append(q, k, v, step.positions, step.slots, rotary, k_cache, v_cache, copies=step.copies)    # once per layer
     out = attend(q, k_cache, v_cache, step.table, cu_seqlens, cached_lens)
 
+A step that checks trees of drafted tokens has, with `step` as above,
+
+    tree = draft_tree(parents, cu_seqlens, cached_lens, max_new)                                          # once per step
+    q = rope_append(q, k, v, tree.positions, step.slots, rotary, k_cache, v_cache, copies=step.copies)    # once per layer
+    out = attend_tree(q, k_cache, v_cache, step.table, cu_seqlens, cached_lens, tree.positions, tree.seen)
+    kept = accept_path(tokens, parents, choices, cu_seqlens, cached_lens, ...)                            # behind the model
+    keep_path(caches, step.table, cu_seqlens, cached_lens, kept.path)                                     # all layers
+
 All of it is enqueued on the current torch stream, nothing waits for the GPU, and lengths are read there; outputs and the
 workspace are torch tensors.  There is no CPU fallback: loading raises if the library has not been built.  There is no backward
 pass either: where a graph is recorded, tensors that require grad are refused (serve under `torch.no_grad()`).
@@ -63,6 +71,15 @@ def load_library():
     lib.attn_attend.restype = ctypes.c_int
     lib.attn_attend.argtypes = [shape, i32, i64, i32, i32, vp, i64, vp, vp, vp, vp, vp, ctypes.c_float, i32, i32, i32, vp,
                                 i64, vp, vp, ctypes.c_size_t, vp]
+    lib.attn_draft_tree.restype = ctypes.c_int
+    lib.attn_draft_tree.argtypes = [i32, i64, i32, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.attn_attend_tree.restype = ctypes.c_int
+    lib.attn_attend_tree.argtypes = [shape, i32, i64, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i32, ctypes.c_float, i32, i32,
+                                     i32, vp, i64, vp, vp, ctypes.c_size_t, vp]
+    lib.attn_accept_path.restype = ctypes.c_int
+    lib.attn_accept_path.argtypes = [i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.attn_keep_path.restype = ctypes.c_int
+    lib.attn_keep_path.argtypes = [shape, i32, i64, i32, i32, i32, ctypes.POINTER(vp), vp, vp, vp, vp, vp]
     lib.attn_last_error.restype = ctypes.c_char_p
     lib.attn_last_error.argtypes = []
     _lib = lib
@@ -153,3 +170,48 @@ def attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, *, scale: Option
     number of new tokens of any sequence, picks the faster kernel (0: not known)."""
     return (_binding or _native()).attend(q, k_cache, v_cache, table, cu_seqlens, cached_lens, scale, window, sinks, max_new, out,
                                           return_lse)
+
+
+class Tree(NamedTuple):
+    """What `draft_tree` returns; device tensors."""
+    positions: "torch.Tensor"  # [total_tokens] int32
+    seen: "torch.Tensor"       # [total_tokens, ceil(max_new / 32)] int32: bit j: the token sees new token j of its sequence
+
+
+def draft_tree(parents, cu_seqlens, cached_lens, max_new: int, *, window: int = 0, sinks: int = 0) -> Tree:
+    """Positions and visibility of a step's trees.  `parents` [tokens] int32: the index in its sequence of the token in front of
+    each, -1 where only cached ones are; `max_new` at least the longest sequence's new tokens, at most 1024.  Layers with a
+    sliding window take bits of their own."""
+    return Tree._make((_binding or _native()).draft_tree(parents, cu_seqlens, cached_lens, max_new, window, sinks))
+
+
+def attend_tree(q, k_cache, v_cache, table, cu_seqlens, cached_lens, positions, seen, *, scale: Optional[float] = None,
+                window: int = 0, sinks: int = 0, max_new: int = 0, out=None, return_lse: bool = False):
+    """`attend` where the new tokens are trees: cached keys are seen by `positions`, a sequence's new tokens by the bits of
+    `seen`, which need not come from `draft_tree`: a row may have any bits up to its own token's, or none."""
+    return (_binding or _native()).attend_tree(q, k_cache, v_cache, table, cu_seqlens, cached_lens, positions, seen, scale, window,
+                                               sinks, max_new, out, return_lse)
+
+
+class Accepted(NamedTuple):
+    """What `accept_path` returns; device tensors of int32."""
+    path: "torch.Tensor"         # [total_tokens]: at cu_seqlens[b] + k the k-th kept token of sequence b, -1 behind the last
+    counts: "torch.Tensor"       # [batch]: kept tokens
+    next_tokens: "torch.Tensor"  # [batch]: the token chosen behind the last kept one
+    kept_lens: "torch.Tensor"    # [batch]: cached tokens of the next step
+    n_free: Optional["torch.Tensor"]  # [1]: length of the free list with the blocks that came back; None without a table
+
+
+def accept_path(tokens, parents, choices, cu_seqlens, cached_lens, *, block_size: int = 0, table=None, free_blocks=None,
+                n_free=None) -> Accepted:
+    """The branch of each tree that `choices` agrees with: its first token, and from there on the first child that is the token
+    chosen behind its parent.  With `table`, `free_blocks` and `n_free` (as `assign_blocks` left them: `step.table`, the list,
+    `step.counts[:1]`) blocks of tokens that are not kept are put back on the list, in place."""
+    return Accepted._make((_binding or _native()).accept_path(tokens, parents, choices, cu_seqlens, cached_lens, block_size, table,
+                                                              free_blocks, n_free))
+
+
+def keep_path(caches, table, cu_seqlens, cached_lens, path) -> None:
+    """Keys and values of the kept tokens to where a chain of tokens has them, in every cache of the list `caches` (k_cache and
+    v_cache of all layers), in place.  `cached_lens` are the step's."""
+    (_binding or _native()).keep_path(caches, table, cu_seqlens, cached_lens, path)

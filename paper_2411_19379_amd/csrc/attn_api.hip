@@ -1,4 +1,5 @@
 // Entry points of the attention operators: argument checks and launches.  Nothing here allocates or synchronises.
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -96,6 +97,15 @@ int check_attend_batch(const attn_shape_t *s, int32_t batch, int64_t total_token
     return ATTN_OK;
 }
 
+int check_tree_words(int32_t words)
+{
+    if (words < 1 || words > kMostTreeWords)
+        return fail(ATTN_ERR_UNSUPPORTED_SHAPE, "a tree has 1 to 32 words of bits, up to 1024 tokens");
+    return ATTN_OK;
+}
+
+constexpr int kMostCaches = 256;
+
 }  // namespace
 
 extern "C" const char *attn_last_error(void) { return g_error.c_str(); }
@@ -186,11 +196,11 @@ extern "C" int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, in
     return ATTN_OK;
 }
 
-extern "C" int attn_attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks,
-                           int32_t max_blocks, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
-                           const int32_t *table, const int32_t *cu_seqlens, const int32_t *cached_lens, float scale,
-                           int32_t window, int32_t sinks, int32_t max_new, void *out, int64_t out_stride, float *lse,
-                           void *workspace, size_t workspace_bytes, void *hip_stream)
+static int attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks, int32_t max_blocks,
+                  const void *q, int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
+                  const int32_t *cu_seqlens, const int32_t *cached_lens, const AttnTrees &trees, float scale, int32_t window,
+                  int32_t sinks, int32_t max_new, void *out, int64_t out_stride, float *lse, void *workspace,
+                  size_t workspace_bytes, void *hip_stream)
 {
     int rc = check_attend_shape(shape);
     if (rc == ATTN_OK)
@@ -225,5 +235,128 @@ extern "C" int attn_attend(const attn_shape_t *shape, int32_t batch, int64_t tot
     }
     return hip_status(launch_attn_attend(*shape, batch, total_tokens, n_blocks, max_blocks, q, q_stride, k_cache, v_cache,
                                          table, cu_seqlens, cached_lens, scale, window, sinks, max_new, out, out_stride, lse,
-                                         workspace, static_cast<hipStream_t>(hip_stream)));
+                                         workspace, static_cast<hipStream_t>(hip_stream), trees));
+}
+
+extern "C" int attn_attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks,
+                           int32_t max_blocks, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                           const int32_t *table, const int32_t *cu_seqlens, const int32_t *cached_lens, float scale,
+                           int32_t window, int32_t sinks, int32_t max_new, void *out, int64_t out_stride, float *lse,
+                           void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    return attend(shape, batch, total_tokens, n_blocks, max_blocks, q, q_stride, k_cache, v_cache, table, cu_seqlens, cached_lens,
+                  AttnTrees(), scale, window, sinks, max_new, out, out_stride, lse, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" int attn_attend_tree(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks,
+                                int32_t max_blocks, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                                const int32_t *table, const int32_t *cu_seqlens, const int32_t *cached_lens,
+                                const int32_t *positions, const int32_t *seen, int32_t words, float scale, int32_t window,
+                                int32_t sinks, int32_t max_new, void *out, int64_t out_stride, float *lse, void *workspace,
+                                size_t workspace_bytes, void *hip_stream)
+{
+    int rc = check_tree_words(words);
+    if (rc == ATTN_OK && total_tokens > 0 && (!positions || !seen))
+        rc = fail(ATTN_ERR_INVALID_ARG, "positions or seen is NULL");
+    if (rc != ATTN_OK)
+        return rc;
+    AttnTrees trees;
+    trees.positions = positions, trees.seen = seen, trees.words = words;
+    return attend(shape, batch, total_tokens, n_blocks, max_blocks, q, q_stride, k_cache, v_cache, table, cu_seqlens, cached_lens,
+                  trees, scale, window, sinks, max_new, out, out_stride, lse, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" int attn_draft_tree(int32_t batch, int64_t total_tokens, int32_t words, const int32_t *parents,
+                               const int32_t *cu_seqlens, const int32_t *cached_lens, int32_t window, int32_t sinks,
+                               int32_t *positions, int32_t *seen, void *hip_stream)
+{
+    int rc = check_batch(batch, total_tokens);
+    if (rc == ATTN_OK)
+        rc = check_tree_words(words);
+    if (rc != ATTN_OK)
+        return rc;
+    if (window < 0 || sinks < 0)
+        return fail(ATTN_ERR_INVALID_ARG, "window and sinks must not be negative");
+    if (total_tokens == 0)
+        return ATTN_OK;
+    if (batch == 0)
+        return fail(ATTN_ERR_INVALID_ARG, "tokens without sequences");
+    if (!parents || !cu_seqlens || !cached_lens || !positions || !seen)
+        return fail(ATTN_ERR_INVALID_ARG, "a required pointer is NULL");
+    return hip_status(launch_attn_draft_tree(batch, total_tokens, words, parents, cu_seqlens, cached_lens, window, sinks, positions,
+                                             seen, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" int attn_accept_path(int32_t batch, int32_t block_size, int32_t max_blocks, int64_t total_tokens,
+                                const int32_t *tokens, const int32_t *parents, const int32_t *choices,
+                                const int32_t *cu_seqlens, const int32_t *cached_lens, int32_t *path, int32_t *counts,
+                                int32_t *next_tokens, int32_t *kept_lens, const int32_t *table, int32_t *free_blocks,
+                                int32_t free_capacity, const int32_t *n_free, int32_t *n_free_out, void *hip_stream)
+{
+    const int rc = check_batch(batch, total_tokens);
+    if (rc != ATTN_OK)
+        return rc;
+    if (batch == 0)
+        return total_tokens == 0 ? ATTN_OK : fail(ATTN_ERR_INVALID_ARG, "tokens without sequences");
+    if (!cu_seqlens || !cached_lens || !counts || !next_tokens || !kept_lens)
+        return fail(ATTN_ERR_INVALID_ARG, "a required pointer is NULL");
+    if (total_tokens > 0 && (!tokens || !parents || !choices || !path))
+        return fail(ATTN_ERR_INVALID_ARG, "tokens, parents, choices and path are required where there are tokens");
+    int log2_bs = 0;
+    if (table) {
+        if (block_size < 1 || block_size > 1024 || (block_size & (block_size - 1)) != 0)
+            return fail(ATTN_ERR_UNSUPPORTED_SHAPE, "block_size must be a power of two up to 1024");
+        if (max_blocks < 1 || free_capacity < 0)
+            return fail(ATTN_ERR_INVALID_ARG, "max_blocks must be positive, free_capacity not negative");
+        if (!n_free || !n_free_out || (free_capacity > 0 && !free_blocks))
+            return fail(ATTN_ERR_INVALID_ARG, "free_blocks, n_free and n_free_out are required with a table");
+        if (n_free == n_free_out)
+            return fail(ATTN_ERR_INVALID_ARG, "n_free_out must not be n_free: all threads read n_free");
+        log2_bs = __builtin_ctz((unsigned)block_size);
+    }
+    return hip_status(launch_attn_accept(batch, log2_bs, max_blocks, total_tokens, tokens, parents, choices, cu_seqlens, cached_lens,
+                                         table, free_blocks, n_free, free_capacity, path, counts, next_tokens, kept_lens,
+                                         n_free_out, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" int attn_keep_path(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks,
+                              int32_t max_blocks, int32_t n_caches, void *const *caches, const int32_t *table,
+                              const int32_t *cu_seqlens, const int32_t *cached_lens, const int32_t *path, void *hip_stream)
+{
+    int rc = check_shape(shape);
+    if (rc == ATTN_OK)
+        rc = check_batch(batch, total_tokens);
+    if (rc == ATTN_OK)
+        rc = check_cache(shape, n_blocks);
+    if (rc != ATTN_OK)
+        return rc;
+    const attn_shape_t &s = *shape;
+    if (s.head_dim % 8 != 0 || s.head_dim > 256)
+        return fail(ATTN_ERR_UNSUPPORTED_SHAPE, "attn_keep_path handles a head_dim that is a multiple of 8 up to 256");
+    if (n_caches < 0 || n_caches > kMostCaches)
+        return fail(ATTN_ERR_UNSUPPORTED_SHAPE, "at most 256 caches per call");
+    if (max_blocks < 1 || (n_caches > 0 && !caches))
+        return fail(ATTN_ERR_INVALID_ARG, "max_blocks must be positive, caches must not be NULL");
+    const unsigned char *at[kMostCaches];
+    for (int c = 0; c < n_caches; ++c) {
+        if (!caches[c])
+            return fail(ATTN_ERR_INVALID_ARG, "a cache is NULL");
+        if (!aligned16(caches[c]))
+            return fail(ATTN_ERR_MISALIGNED, "device pointers must be 16-byte aligned");
+        at[c] = static_cast<const unsigned char *>(caches[c]);
+    }
+    // rows that move in two caches at once would be overwritten before they have been read
+    const int64_t bytes = (int64_t)n_blocks * s.n_kv_heads * s.block_size * s.head_dim * (s.io_dtype == ATTN_DT_F32 ? 4 : 2);
+    std::sort(at, at + n_caches);
+    for (int c = 1; c < n_caches; ++c)
+        if (at[c] - at[c - 1] < bytes)
+            return fail(ATTN_ERR_INVALID_ARG, "two caches overlap");
+    if (total_tokens == 0 || n_caches == 0)
+        return ATTN_OK;
+    if (batch == 0)
+        return fail(ATTN_ERR_INVALID_ARG, "tokens without sequences");
+    if (!table || !cu_seqlens || !cached_lens || !path)
+        return fail(ATTN_ERR_INVALID_ARG, "a required pointer is NULL");
+    return hip_status(launch_attn_keep(s, batch, total_tokens, n_blocks, max_blocks, n_caches, caches, table, cu_seqlens,
+                                       cached_lens, path, static_cast<hipStream_t>(hip_stream)));
 }

@@ -65,7 +65,7 @@ template <int D> struct ChunkTile {
     static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ v_turn(r)) << 4); }
 };
 
-template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 * NW, D == 64 ? 4 : 2) void attn_chunk_kernel(AttendArgs a)
+template <typename E, int D, int NW, bool WIDE, bool TREE> __global__ __launch_bounds__(64 * NW, D == 64 ? 4 : 2) void attn_chunk_kernel(AttendArgs a)
 {
     typedef ChunkTile<D> Tile;
     constexpr int ROWS = 32 * NW, PIECES = Tile::kPieces;
@@ -86,7 +86,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
-    const KeyRange keys = key_range<kChunkKeys>(a, s, r0, ROWS);
+    const KeyRange keys = key_range<kChunkKeys, TREE>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits);
     const int n = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits) - step_begin;
     const int end = keys.end;
@@ -95,9 +95,9 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     const int row = r0 + 32 * wave + l % 32;
     const bool wave_works = r0 + 32 * wave < s.rows, row_works = row < s.rows;
     const int token = row_works ? row / a.group : 0, head = kv_head * a.group + (row_works ? row - token * a.group : 0);
-    const int pos = s.cached + token;
+    const int pos = TREE && row_works ? tree_position(a, s, token) : s.cached + token;
     const int wave_last = r0 + 32 * wave + 31 < s.rows ? r0 + 32 * wave + 31 : s.rows - 1;
-    const int wave_pos0 = s.cached + (wave_works ? (r0 + 32 * wave) / a.group : 0);
+    const int wave_pos0 = TREE ? s.cached - 1 : s.cached + (wave_works ? (r0 + 32 * wave) / a.group : 0);
     const int wave_pos1 = s.cached + (wave_works ? wave_last / a.group : 0);
     uint4 qf[D / 16];
 #pragma unroll
@@ -121,7 +121,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     // not exist is read from the cache's first rows, so that no load waits for a branch: what it gets as K comes to nothing in
     // the softmax, as V it is cleared.
     const int load_row = wave * KEYS + l / PIECES, load_at = l % PIECES;
-    const SeenTiles seen_by_all(a, keys.pos0, keys.pos1, kChunkKeys), seen_by_wave(a, wave_pos0, wave_pos1, kChunkKeys);
+    const SeenTiles seen_by_all(a, keys.pos0 - (TREE ? 1 : 0), keys.pos1, kChunkKeys), seen_by_wave(a, wave_pos0, wave_pos1, kChunkKeys);
     const int32_t *const table = reinterpret_cast<const int32_t *>(own_pointer(a.table + (int64_t)it.seq * a.max_blocks));
     const unsigned char *const k_cache = own_pointer(a.k_cache), *const v_cache = own_pointer(a.v_cache);
     const int bs_mask = (1 << a.log2_bs) - 1;
@@ -259,7 +259,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
             }
             const float p = read_from(key % 2 ? E::hi(two) : E::lo(two), l % 32 + 32 * from);
             const int j = j0 + key, e = j >> a.log2_bs, cr = cache_row(a, j < end && e < a.max_blocks ? table[e] : -1, kv_head, j);
-            const uint32_t sees_it = row_works && cr >= 0 && sees(a, pos, j) ? ~0u : 0u;
+            const uint32_t sees_it = row_works && cr >= 0 && sees<TREE>(a, s, pos, token, j) ? ~0u : 0u;
             const uint16_t *v_of = reinterpret_cast<const uint16_t *>(v_cache) + (int64_t)(cr < 0 ? 0 : cr) * D;
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
@@ -276,7 +276,7 @@ template <typename E, int D, int NW, bool WIDE> __global__ __launch_bounds__(64 
     auto softmax = [&](int t, int j0) __attribute__((always_inline)) {
         const uint64_t exist = __ballot(lds_exist[(t & 3) * kChunkKeys + (WIDE ? l & -KEYS : l)] != 0);
         if (!seen_by_wave.all(j0) || exist != ~0ull) {
-            const uint64_t keys_seen = seen_keys(a, unknown(pos), j0, exist);
+            const uint64_t keys_seen = seen_keys<TREE>(a, s, unknown(pos), unknown(token), j0, exist);
             seen = seen || keys_seen != 0;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
@@ -432,7 +432,7 @@ template <int D> struct FewTile {
     static __device__ __forceinline__ int v_at(int r, int c) { return r * D * 2 + ((c ^ (D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1)) << 4); }
 };
 
-template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
+template <typename E, int D, int RB, bool WIDE, bool TREE> __global__ __launch_bounds__(64 * kFewWaves, RB * D > 128 ? 1 : 2) void attn_few_kernel(AttendArgs a)
 {
     typedef FewTile<D> Tile;
     constexpr int ROWS = 16 * RB, PIECES = Tile::kPieces;
@@ -449,7 +449,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
-    const KeyRange keys = key_range<kFewKeys>(a, s, r0, ROWS);
+    const KeyRange keys = key_range<kFewKeys, TREE>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
     const int end = keys.end;
 
@@ -462,7 +462,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
         row_works[rb] = row < s.rows;
         token[rb] = row_works[rb] ? row / a.group : 0;
         head[rb] = kv_head * a.group + (row_works[rb] ? row - token[rb] * a.group : 0);
-        pos[rb] = s.cached + token[rb];
+        pos[rb] = TREE && row_works[rb] ? tree_position(a, s, token[rb]) : s.cached + token[rb];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             qf[rb][ks] = make_uint4(0, 0, 0, 0);
@@ -547,7 +547,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
         request(step_begin + wave);
         look_up(step_begin + wave + kFewWaves);
     }
-    const SeenTiles seen_tiles(a, keys.pos0, keys.pos1, kFewKeys);
+    const SeenTiles seen_tiles(a, keys.pos0 - (TREE ? 1 : 0), keys.pos1, kFewKeys);
     for (int step = step_begin + wave; step < step_end; step += kFewWaves) {
         const int j0 = keys.tile(step) * kFewKeys;
         const bool part_seen = !seen_tiles.all(j0);
@@ -598,7 +598,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             if (partly) {
-                const uint32_t keys_seen = (uint32_t)seen_keys(a, pos[rb], j0, exist), mine = keys_seen >> (4 * quarter);
+                const uint32_t keys_seen = (uint32_t)seen_keys<TREE>(a, s, pos[rb], token[rb], j0, exist), mine = keys_seen >> (4 * quarter);
                 seen[rb] = seen[rb] || keys_seen != 0;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
@@ -657,7 +657,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
                 for (int e = 0; e < 8; ++e)
                     p = e == e_of ? st[rb][e / 4][e % 4] : p;
                 p = read_from(p, l % 16 + 16 * from);
-                const uint32_t sees_it = row_works[rb] && cr >= 0 && sees(a, pos[rb], j0 + key) ? ~0u : 0u;
+                const uint32_t sees_it = row_works[rb] && cr >= 0 && sees<TREE>(a, s, pos[rb], token[rb], j0 + key) ? ~0u : 0u;
 #pragma unroll
                 for (int db = 0; db < D / 16; ++db) {
                     float v[4];
@@ -742,7 +742,7 @@ template <typename E, int D, int RB, bool WIDE> __global__ __launch_bounds__(64 
 constexpr int kF32Keys = 32;
 constexpr int kF32Waves = 4;
 
-template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_kernel(AttendArgs a)
+template <int D, bool TREE> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_kernel(AttendArgs a)
 {
     constexpr int NT = 64 * kF32Waves, ROWS = 16 * kF32Waves;
     constexpr int PIECES = D / 4, LOADS = kF32Keys * PIECES / NT, ROWS_PER_LOAD = NT / PIECES;
@@ -760,14 +760,14 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         return;
     const Seq s = load_seq(a, it.seq);
     const int r0 = it.tile * ROWS;
-    const KeyRange keys = key_range<kF32Keys>(a, s, r0, ROWS);
+    const KeyRange keys = key_range<kF32Keys, TREE>(a, s, r0, ROWS);
     const int step_begin = (int)((int64_t)keys.n * it.split / it.n_splits), step_end = (int)((int64_t)keys.n * (it.split + 1) / it.n_splits);
     const int end = keys.end;
 
     const int row = r0 + 16 * wave + l % 16;
     const bool wave_works = r0 + 16 * wave < s.rows, row_works = row < s.rows;
     const int token = row_works ? row / a.group : 0, head = kv_head * a.group + (row_works ? row - token * a.group : 0);
-    const int pos = s.cached + token;
+    const int pos = TREE && row_works ? tree_position(a, s, token) : s.cached + token;
     f32x4 qf[D / 16];
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
@@ -816,7 +816,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks)
         qf[ks] = unknown(qf[ks]);
-    const SeenTiles seen_tiles(a, keys.pos0, keys.pos1, kF32Keys);
+    const SeenTiles seen_tiles(a, keys.pos0 - (TREE ? 1 : 0), keys.pos1, kF32Keys);
     for (int step = step_begin; step < step_end; ++step) {
         const int j0 = keys.tile(step) * kF32Keys;
         const bool part_seen = !seen_tiles.all(j0);
@@ -869,7 +869,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
         const uint32_t exist = (uint32_t)__ballot((f & 1) != 0), bad = (uint32_t)__ballot((f & 2) != 0);
         const bool partly = part_seen || exist != 0xffffffffu;
         if (partly) {
-            const uint32_t keys_seen = (uint32_t)seen_keys(a, pos, j0, exist), mine = keys_seen >> (4 * quarter);
+            const uint32_t keys_seen = (uint32_t)seen_keys<TREE>(a, s, pos, token, j0, exist), mine = keys_seen >> (4 * quarter);
             seen = seen || keys_seen != 0;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -928,7 +928,7 @@ template <int D> __global__ __launch_bounds__(64 * kF32Waves, 2) void attn_f32_k
             for (int e = 0; e < 8; ++e)
                 p = e == e_of ? st[e / 4][e % 4] : p;
             p = read_from(p, l % 16 + 16 * from);
-            const uint32_t sees_it = row_works && cr >= 0 && sees(a, pos, j0 + key) ? ~0u : 0u;
+            const uint32_t sees_it = row_works && cr >= 0 && sees<TREE>(a, s, pos, token, j0 + key) ? ~0u : 0u;
 #pragma unroll
             for (int db = 0; db < D / 16; ++db) {
                 const float4 x = *reinterpret_cast<const float4 *>(v_row + db * 16 + 4 * quarter);
@@ -1165,7 +1165,7 @@ template <int KT> bool may_split(const AttendArgs &a, const Launch &c)
 {
     int64_t steps = ((((int64_t)a.max_blocks << a.log2_bs) + KT - 1) / KT);
     if (a.window > 0) {
-        const int64_t seen = ((int64_t)a.window + c.rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
+        const int64_t seen = ((int64_t)a.window + (a.words > 0 ? 32 * a.words : c.rows / a.group) + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
         steps = seen < steps ? seen : steps;
     }
     return steps + c.min_steps / 2 >= 2 * (int64_t)c.min_steps;
@@ -1193,46 +1193,51 @@ template <typename K> hipError_t lds_limit(K kernel, size_t lds)
                        : hipSuccess;
 }
 
-template <typename E, int D, int RB> hipError_t launch_few(const AttendArgs &a, const Launch &c, hipStream_t stream)
+template <typename K> hipError_t launch_on(K kernel, const AttendArgs &a, const Launch &c, int threads, size_t lds, hipStream_t stream)
 {
-    constexpr size_t v = (size_t)kFewWaves * FewTile<D>::kBytes, o = (size_t)kFewWaves * 16 * (D + 4 + 2) * sizeof(float);
-    constexpr size_t lds = v > o ? v : o;
-    if (1 << a.log2_bs >= 16)
-        hipLaunchKernelGGL((attn_few_kernel<E, D, RB, true>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
-    else
-        hipLaunchKernelGGL((attn_few_kernel<E, D, RB, false>), dim3((unsigned)c.grid), dim3(64 * kFewWaves), lds, stream, a);
+    const hipError_t e = lds_limit(kernel, lds);
+    if (e != hipSuccess)
+        return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)c.grid), dim3(threads), lds, stream, a);
     return hipGetLastError();
 }
 
-template <typename E, int D> hipError_t launch16(const AttendArgs &a, const Launch &c, bool chunk, hipStream_t stream)
+template <typename E, int D, int RB, bool TREE> hipError_t launch_few(const AttendArgs &a, const Launch &c, hipStream_t stream)
+{
+    constexpr size_t v = (size_t)kFewWaves * FewTile<D>::kBytes, o = (size_t)kFewWaves * 16 * (D + 4 + 2) * sizeof(float);
+    constexpr size_t lds = v > o ? v : o;
+    return 1 << a.log2_bs >= 16 ? launch_on(attn_few_kernel<E, D, RB, true, TREE>, a, c, 64 * kFewWaves, lds, stream)
+                                : launch_on(attn_few_kernel<E, D, RB, false, TREE>, a, c, 64 * kFewWaves, lds, stream);
+}
+
+template <typename E, int D, bool TREE> hipError_t launch16(const AttendArgs &a, const Launch &c, bool chunk, hipStream_t stream)
 {
     hipError_t e;
     if (chunk) {
         constexpr size_t lds = 2 * kChunkBuffers * (size_t)ChunkTile<D>::kBytes + 8 * kChunkKeys * sizeof(int);
-        const bool wide = 1 << a.log2_bs >= kChunkKeys / kChunkWaves;
-        e = wide ? lds_limit(attn_chunk_kernel<E, D, kChunkWaves, true>, lds) : lds_limit(attn_chunk_kernel<E, D, kChunkWaves, false>, lds);
-        if (e != hipSuccess)
-            return e;
-        if (wide)
-            hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves, true>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
-        else
-            hipLaunchKernelGGL((attn_chunk_kernel<E, D, kChunkWaves, false>), dim3((unsigned)c.grid), dim3(64 * kChunkWaves), lds, stream, a);
-        e = hipGetLastError();
+        e = 1 << a.log2_bs >= kChunkKeys / kChunkWaves ? launch_on(attn_chunk_kernel<E, D, kChunkWaves, true, TREE>, a, c, 64 * kChunkWaves, lds, stream)
+                                                       : launch_on(attn_chunk_kernel<E, D, kChunkWaves, false, TREE>, a, c, 64 * kChunkWaves, lds, stream);
     } else {
-        e = c.rows == 16 ? launch_few<E, D, 1>(a, c, stream) : launch_few<E, D, 2>(a, c, stream);
+        e = c.rows == 16 ? launch_few<E, D, 1, TREE>(a, c, stream) : launch_few<E, D, 2, TREE>(a, c, stream);
     }
     return e != hipSuccess ? e : join<E, D>(a, c, !chunk, false, stream);
 }
 
-template <int D> hipError_t launch_f32(const AttendArgs &a, const Launch &c, hipStream_t stream)
+template <int D, bool TREE> hipError_t launch_f32(const AttendArgs &a, const Launch &c, hipStream_t stream)
 {
     constexpr size_t lds = 4 * (size_t)kF32Keys * (D + 4) * sizeof(float) + 2 * kF32Keys * sizeof(int);
-    const hipError_t limit = lds_limit(attn_f32_kernel<D>, lds);
-    if (limit != hipSuccess)
-        return limit;
-    hipLaunchKernelGGL((attn_f32_kernel<D>), dim3((unsigned)c.grid), dim3(64 * kF32Waves), lds, stream, a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_on(attn_f32_kernel<D, TREE>, a, c, 64 * kF32Waves, lds, stream);
     return e != hipSuccess ? e : join<float, D>(a, c, false, true, stream);
+}
+
+template <bool TREE> hipError_t launch_type(const attn_shape_t &s, const AttendArgs &a, const Choice &c, hipStream_t stream)
+{
+    const Launch &u = c.launch;
+    if (s.io_dtype == ATTN_DT_F32)
+        return s.head_dim == 64 ? launch_f32<64, TREE>(a, u, stream) : launch_f32<128, TREE>(a, u, stream);
+    if (s.io_dtype == ATTN_DT_BF16)
+        return s.head_dim == 64 ? launch16<Bf16, 64, TREE>(a, u, c.chunk, stream) : launch16<Bf16, 128, TREE>(a, u, c.chunk, stream);
+    return s.head_dim == 64 ? launch16<F16, 64, TREE>(a, u, c.chunk, stream) : launch16<F16, 128, TREE>(a, u, c.chunk, stream);
 }
 
 }  // namespace
@@ -1247,7 +1252,7 @@ size_t attn_attend_workspace(const attn_shape_t &s, int batch, int64_t T, int ma
 hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
                               int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
                               const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
-                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream)
+                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream, const AttnTrees &trees)
 {
     const Choice c = choose(s, batch, T, max_new);
     const Launch &u = c.launch;
@@ -1283,9 +1288,8 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
     a.target = u.target;
     a.min_steps = u.min_steps;
     a.half_steps = u.half_steps;
-    if (s.io_dtype == ATTN_DT_F32)
-        return s.head_dim == 64 ? launch_f32<64>(a, u, stream) : launch_f32<128>(a, u, stream);
-    if (s.io_dtype == ATTN_DT_BF16)
-        return s.head_dim == 64 ? launch16<Bf16, 64>(a, u, c.chunk, stream) : launch16<Bf16, 128>(a, u, c.chunk, stream);
-    return s.head_dim == 64 ? launch16<F16, 64>(a, u, c.chunk, stream) : launch16<F16, 128>(a, u, c.chunk, stream);
+    a.positions = trees.positions;
+    a.seen = trees.seen;
+    a.words = trees.words;
+    return a.words > 0 ? launch_type<true>(s, a, c, stream) : launch_type<false>(s, a, c, stream);
 }

@@ -116,6 +116,9 @@ struct AttendArgs {
     uint32_t target;        // workgroups that keep the GPU busy
     int32_t min_steps;      // a workgroup gets no fewer steps of keys than this if it can help it
     int32_t half_steps;     // up to so many it gets what it would get if half of the workgroups shared them
+    // trees of new tokens; words is 0 where a sequence's new tokens follow one another
+    const int32_t *positions, *seen;  // [T], [T, words]: bit j of row i: the query of new token i sees new token j
+    int32_t words;
 };
 
 // ---------------------------------------------------------------- sequences
@@ -153,11 +156,12 @@ struct KeyRange {
     int n;           // tiles in all
     __device__ __forceinline__ int tile(int step) const { return step < n_sink ? step : near + step - n_sink; }
 };
-template <int KT> __device__ __forceinline__ KeyRange key_range(const AttendArgs &a, const Seq &s, int r0, int rows)
+template <int KT, bool TREE = false> __device__ __forceinline__ KeyRange key_range(const AttendArgs &a, const Seq &s, int r0, int rows)
 {
     KeyRange k;
     const int last = r0 + rows < s.rows ? r0 + rows - 1 : s.rows - 1;
-    k.pos0 = s.cached + r0 / a.group;
+    // a tree's tokens lie one behind the other in the cache, and any of them may be the first behind the cached ones by its position
+    k.pos0 = TREE ? s.cached : s.cached + r0 / a.group;
     k.pos1 = s.cached + last / a.group;
     const int most = table_end(a);
     k.end = k.pos1 < most ? k.pos1 + 1 : most;
@@ -173,7 +177,7 @@ template <int KT> __device__ __forceinline__ KeyRange key_range(const AttendArgs
 // place for, and no more than a window has.  The host computes the same bounds for any sequence (may_split).
 template <int KT> __device__ __forceinline__ int window_steps(const AttendArgs &a, int rows)
 {
-    const int64_t near = ((int64_t)a.window + rows / a.group + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
+    const int64_t near = ((int64_t)a.window + (a.words > 0 ? 32 * a.words : rows / a.group) + 1) / KT + 2 + ((int64_t)a.sinks + KT - 1) / KT;
     return a.window > 0 && near < 0x7fffffff ? (int)near : 0x7fffffff;
 }
 
@@ -190,6 +194,37 @@ __device__ __forceinline__ uint64_t seen_keys(const AttendArgs &a, int pos, int 
         m &= ~first_bits(pos - j0 - a.window + 1) | first_bits(a.sinks - j0);
     return m;
 }
+// Of a tree's token the query sees cached keys by its position, which lies between the first new one and the one that it would
+// have in a chain, and new ones by its bits, up to its own.
+__device__ __forceinline__ int tree_position(const AttendArgs &a, const Seq &s, int token)
+{
+    const int p = a.positions[s.start + token], most = s.cached + token;
+    return p < s.cached ? s.cached : p > most ? most : p;
+}
+// The bits of new tokens [first, first + 64); `first` may be negative.
+__device__ __forceinline__ uint64_t tree_bits(const AttendArgs &a, const Seq &s, int token, int first)
+{
+    const int32_t *const row = a.seen + (int64_t)(s.start + token) * a.words;
+    const int w = first >> 5, shift = first & 31;
+    uint32_t word[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        word[k] = (uint32_t)(w + k) < (uint32_t)a.words ? (uint32_t)row[w + k] : 0u;
+    const uint64_t low = (uint64_t)word[1] << 32 | word[0];
+    const uint64_t bits = shift == 0 ? low : low >> shift | (uint64_t)word[2] << (64 - shift);
+    return bits & first_bits(token - first + 1);
+}
+template <bool TREE> __device__ __forceinline__ uint64_t seen_keys(const AttendArgs &a, const Seq &s, int pos, int token, int j0, uint64_t exist)
+{
+    if (!TREE)
+        return seen_keys(a, pos, j0, exist);
+    const uint64_t cached = seen_keys(a, pos, j0, first_bits(s.cached - j0));
+    return exist & (s.cached - j0 < 64 ? cached | tree_bits(a, s, token, j0 - s.cached) : cached);
+}
+template <bool TREE> __device__ __forceinline__ bool sees(const AttendArgs &a, const Seq &s, int pos, int token, int j)
+{
+    return TREE && j >= s.cached ? (tree_bits(a, s, token, j - s.cached) & 1) != 0 : sees(a, pos, j);
+}
 // The score, or minus infinity (a weight of 0 in any case) if `bit` of the keys that are seen is not set: two bit operations and
 // no condition register.
 __device__ __forceinline__ float seen_score(float score, uint32_t keys, int bit)
@@ -198,7 +233,8 @@ __device__ __forceinline__ float seen_score(float score, uint32_t keys, int bit)
     return __uint_as_float((__float_as_uint(score) & is) | (0xff800000u & ~is));
 }
 
-// Of which tiles of n keys every row at positions pos0..pos1 sees every key.
+// Of which tiles of n keys every row at positions pos0..pos1 sees every key.  (Of a tree's rows every one sees the cached keys and,
+// for all that is known here, no other: pos0 is the last cached position.)
 struct SeenTiles {
     int last, behind, sinks;  // first keys: up to `last` and behind `behind`, or up to `sinks`
     __device__ __forceinline__ SeenTiles(const AttendArgs &a, int pos0, int pos1, int n)
@@ -446,8 +482,25 @@ hipError_t launch_attn_rope(const attn_shape_t &s, int64_t T, int batch, int n_b
                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int32_t *positions,
                             const int64_t *slots, const float *rotary, int max_positions, int rotary_dim, bool interleaved,
                             const int32_t *copies, void *q_out, void *k_cache, void *v_cache, hipStream_t stream);
+// The trees of a batch's new tokens; none (0 words): they follow one another.
+struct AttnTrees {
+    const int32_t *positions = nullptr, *seen = nullptr;
+    int32_t words = 0;
+};
 hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
                               int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
                               const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
-                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream);
+                              void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream,
+                              const AttnTrees &trees = AttnTrees());
+constexpr int kMostTreeWords = 32;   // a tree has up to 1024 tokens
+constexpr int kCachesPerLaunch = 32; // their pointers travel in the kernel's arguments
+hipError_t launch_attn_draft_tree(int batch, int64_t T, int words, const int32_t *parents, const int32_t *cu, const int32_t *cached,
+                                  int window, int sinks, int32_t *positions, int32_t *seen, hipStream_t stream);
+hipError_t launch_attn_accept(int batch, int log2_bs, int max_blocks, int64_t T, const int32_t *tokens, const int32_t *parents,
+                              const int32_t *choices, const int32_t *cu, const int32_t *cached, const int32_t *table,
+                              int32_t *free_blocks, const int32_t *n_free, int32_t free_capacity, int32_t *path, int32_t *counts,
+                              int32_t *next_tokens, int32_t *kept_lens, int32_t *n_free_out, hipStream_t stream);
+hipError_t launch_attn_keep(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, int n_caches,
+                            void *const *caches, const int32_t *table, const int32_t *cu, const int32_t *cached,
+                            const int32_t *path, hipStream_t stream);
 size_t attn_attend_workspace(const attn_shape_t &s, int batch, int64_t T, int max_new);
