@@ -55,11 +55,34 @@ def build_attention(verbose: bool = False) -> str:
     return ATTN_LIB_PATH
 
 
+REC_LIB_PATH = os.path.join(_PKG, "libgated_recurrence.so")
+REC_SOURCES = ["rec_api.hip", "rec_scan.hip", "rec_step.hip"]
+
+
+def build_recurrence(verbose: bool = False) -> str:
+    """The gated recurrent layers' operators."""
+    srcs = [os.path.join(CSRC, s) for s in REC_SOURCES]
+    cmd = ["hipcc", *HIPCC_FLAGS, "-I", os.path.join(_ROOT, "include"), "-I", CSRC, "-o", REC_LIB_PATH, *srcs]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return REC_LIB_PATH
+
+
 ATTN_BINDING_PATH = os.path.join(_PKG, "_attn_binding.so")
+REC_BINDING_PATH = os.path.join(_PKG, "_rec_binding.so")
 
 
 def build_attention_binding(verbose: bool = False) -> str:
     """The binding of these operators to torch tensors: host code over the C ABI, linked against the library beside it."""
+    return _build_binding("attn_binding.cpp", ATTN_LIB_PATH, ATTN_BINDING_PATH, verbose)
+
+
+def build_recurrence_binding(verbose: bool = False) -> str:
+    return _build_binding("rec_binding.cpp", REC_LIB_PATH, REC_BINDING_PATH, verbose)
+
+
+def _build_binding(source: str, library: str, to: str, verbose: bool) -> str:
     import sysconfig
 
     import torch
@@ -70,12 +93,12 @@ def build_attention_binding(verbose: bool = False) -> str:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", "/opt/rocm/include",
            "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(_ROOT, "include"),
-           "-o", ATTN_BINDING_PATH, os.path.join(CSRC, "attn_binding.cpp"), "-L", _PKG, "-l:libattn_cache.so", "-Wl,-rpath,$ORIGIN",
+           "-I", CSRC, "-o", to, os.path.join(CSRC, source), "-L", _PKG, "-l:" + os.path.basename(library), "-Wl,-rpath,$ORIGIN",
            "-L", lib, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    return ATTN_BINDING_PATH
+    return to
 
 
 PEAK_PROBE_PATH = os.path.join(_PKG, "peak_probe")
@@ -96,4 +119,6 @@ if __name__ == "__main__":
     build_prefix_cache(verbose=True)
     build_attention(verbose=True)
     build_attention_binding(verbose=True)
+    build_recurrence(verbose=True)
+    build_recurrence_binding(verbose=True)
     build_peak_probe(verbose=True)
