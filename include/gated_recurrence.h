@@ -34,8 +34,8 @@
  *
  * "device" pointers are HIP device pointers on the current device.  x, r, i, y
  * and dy are [total_tokens, channels] of io_dtype with `..._stride` elements
- * between tokens (at least channels; for instance parts of the rows of one
- * projection), aligned to their type.  Every entry point returns REC_OK (0) or
+ * between tokens (at least channels, at most 2^22; for instance parts of the rows
+ * of one projection), aligned to their type.  Every entry point returns REC_OK (0) or
  * a negative rec_status_t; on error nothing has been enqueued and
  * rec_last_error() returns a message for the calling thread.  Nothing here
  * throws or aborts.

@@ -63,8 +63,8 @@ int check_rows(const rec_shape_t &s, const void *p, int64_t stride, const char *
 {
     if (!p)
         return fail(REC_ERR_INVALID_ARG, what);
-    if (stride < s.channels || stride > (int64_t)1 << 40)
-        return fail(REC_ERR_INVALID_ARG, "a token stride is shorter than the channels, or not a length");
+    if (stride < s.channels || stride > kRecMostStride)
+        return fail(REC_ERR_INVALID_ARG, "a token stride is shorter than the channels, or beyond 2^22");
     if (!aligned(p, s.io_dtype == REC_DT_F32 ? 4 : 2))
         return fail(REC_ERR_MISALIGNED, "a device pointer is not aligned to its type");
     return REC_OK;

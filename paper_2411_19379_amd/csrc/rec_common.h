@@ -4,12 +4,21 @@
 #include "gated_recurrence.h"
 #include "mfma_utils.h"
 
+// Products and sums are put together where it is written, and nowhere else: code that is compiled twice, with and without the ends of
+// sequences in it, rounds alike.
+#pragma clang fp contract(off)
+
 namespace {
 
 constexpr int kRecMaxBatch = 4096;
 
 // LDS is ordered, loads in flight stay in flight
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The value is in a register from here on.  What is computed from it behind is not computed in front (the compiler would do so for
+// all tokens of a wave and have no registers for it), and it has been rounded to fp32 (a product and sum that go to fp16 would be
+// rounded once there, and differently where the same code is compiled with something between the two).
+__device__ __forceinline__ void pin(float &v) { asm volatile("" : "+v"(v)); }
 
 // ---------------------------------------------------------------- V neighbouring channels of a token
 struct RecF32 {
@@ -39,24 +48,55 @@ template <typename E> struct RecRow<E, 2> {
     static __device__ __forceinline__ Raw pack(const float *v) { return E::pack(v[0], v[1]); }
 };
 template <> struct RecRow<RecF32, 1> {
-    typedef float Raw;
-    static __device__ __forceinline__ void unpack(Raw r, float *v) { v[0] = r; }
-    static __device__ __forceinline__ Raw pack(const float *v) { return v[0]; }
+    typedef uint32_t Raw;
+    static __device__ __forceinline__ void unpack(Raw r, float *v) { v[0] = __uint_as_float(r); }
+    static __device__ __forceinline__ Raw pack(const float *v) { return __float_as_uint(v[0]); }
 };
 template <> struct RecRow<RecF32, 2> {
-    typedef float2 Raw;
-    static __device__ __forceinline__ void unpack(Raw r, float *v) { v[0] = r.x, v[1] = r.y; }
-    static __device__ __forceinline__ Raw pack(const float *v) { return make_float2(v[0], v[1]); }
+    typedef uint2 Raw;
+    static __device__ __forceinline__ void unpack(Raw r, float *v) { v[0] = __uint_as_float(r.x), v[1] = __uint_as_float(r.y); }
+    static __device__ __forceinline__ Raw pack(const float *v) { return make_uint2(__float_as_uint(v[0]), __float_as_uint(v[1])); }
 };
 // Channels c .. c + V - 1 of row t.
 template <typename E, int V> __device__ __forceinline__ typename RecRow<E, V>::Raw row_load(const void *base, int64_t t, int64_t stride, int c)
 {
-    return *reinterpret_cast<const typename RecRow<E, V>::Raw *>(static_cast<const unsigned char *>(base) + t * stride * E::kBytes + (uint32_t)c * E::kBytes);
+    return *reinterpret_cast<const typename RecRow<E, V>::Raw *>(static_cast<const unsigned char *>(base) + (t * stride + c) * E::kBytes);
 }
 template <typename E, int V> __device__ __forceinline__ void row_store(void *base, int64_t t, int64_t stride, int c, const float *v)
 {
-    *reinterpret_cast<typename RecRow<E, V>::Raw *>(static_cast<unsigned char *>(base) + t * stride * E::kBytes + (uint32_t)c * E::kBytes) = RecRow<E, V>::pack(v);
+    *reinterpret_cast<typename RecRow<E, V>::Raw *>(static_cast<unsigned char *>(base) + (t * stride + c) * E::kBytes) = RecRow<E, V>::pack(v);
 }
+// The same for a wave's rows, through a descriptor: a row is a uniform offset and a lane's place in it one that does not change, so
+// that no address is computed on the vector ALUs (with pointers these were a quarter of the instructions of a token).  A wave's
+// rows span less than 2^31 bytes, since strides are at most kRecMostStride.
+constexpr int64_t kRecMostStride = 1 << 22;
+template <typename E> struct WaveRows {
+    rsrc_t rows;
+    uint32_t stride;  // bytes
+    // `n` rows from row t on, of `channels` channels
+    __device__ __forceinline__ WaveRows(const void *base, int64_t t, int64_t stride_, int n, int channels)
+        : rows(make_rsrc(static_cast<const unsigned char *>(base) + t * stride_ * E::kBytes, ((uint32_t)(n - 1) * (uint32_t)stride_ + (uint32_t)channels) * E::kBytes)),
+          stride((uint32_t)stride_ * E::kBytes)
+    {
+    }
+    // a lane's offset: channel c of row `row`
+    __device__ __forceinline__ uint32_t at(int row, int c) const { return (uint32_t)row * stride + (uint32_t)c * E::kBytes; }
+    __device__ __forceinline__ void get(uint32_t at, int row, uint16_t &r) const { r = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rows, (int)at, (int)(row * stride), 0); }
+    __device__ __forceinline__ void get(uint32_t at, int row, uint32_t &r) const { r = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rows, (int)at, (int)(row * stride), 0); }
+    __device__ __forceinline__ void get(uint32_t at, int row, uint2 &r) const
+    {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(rows, (int)at, (int)(row * stride), 0);
+        r = make_uint2(v[0], v[1]);
+    }
+    __device__ __forceinline__ void put(uint32_t at, int row, uint16_t r) const { __builtin_amdgcn_raw_buffer_store_b16(r, rows, (int)at, (int)(row * stride), 0); }
+    __device__ __forceinline__ void put(uint32_t at, int row, uint32_t r) const { __builtin_amdgcn_raw_buffer_store_b32(r, rows, (int)at, (int)(row * stride), 0); }
+    __device__ __forceinline__ void put(uint32_t at, int row, uint2 r) const
+    {
+        typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 v = {r.x, r.y};
+        __builtin_amdgcn_raw_buffer_store_b64(v, rows, (int)at, (int)(row * stride), 0);
+    }
+};
 template <int V> __device__ __forceinline__ void state_row_load(const float *base, int64_t row, int channels, int c, float *v)
 {
     RecRow<RecF32, V>::unpack(row_load<RecF32, V>(base, row, channels, c), v);
@@ -73,13 +113,17 @@ __device__ __forceinline__ float decay_rate(float decay, float sharpness)
     return -sharpness * (fmaxf(decay, 0.f) + log1pf(expf(-fabsf(decay)))) * kLog2e;
 }
 __device__ __forceinline__ float sigmoid_fast(float v) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(-kLog2e * v)); }
-// 1 - a^2 = -expm1(2 log a), whose value counts where a is next to 1: a series to the sixth power up to 2 log a = -1/4, where the
-// next term is 5e-8 of it; 1 - a a, which loses two bits at most, behind.  (a - 1 from a in fp32 has lost them all at a = 1 - 2^-24.)
+// 1 - a^2 = -expm1(2 log a), whose value counts where a is next to 1: up to v = -2 log a = 1/4 as v times the polynomial of degree 4
+// that is next to (1 - e^-v) / v there (3e-9 of it, found by exchanging extrema), and 1 - a a, which loses two bits at most, behind.
+// (1 - a from a in fp32 has lost all of them at a = 1 - 2^-24.)
 __device__ __forceinline__ float one_minus_square(float log2_a, float a)
 {
-    const float v = log2_a * -1.38629436111989062f;  // -2 log a
-    const float series = v * (1.f + v * (-1.f / 2 + v * (1.f / 6 + v * (-1.f / 24 + v * (1.f / 120 + v * (-1.f / 720))))));
-    return v < 0.25f ? series : __builtin_fmaf(-a, a, 1.f);
+    const float v = log2_a * -1.38629436111989062f;
+    float near = __builtin_fmaf(v, 0.007510221719597369f, -0.041488954085247894f);
+    near = __builtin_fmaf(v, near, 0.16665081472713647f);
+    near = __builtin_fmaf(v, near, -0.49999950132422216f);
+    near = v * __builtin_fmaf(v, near, 1.f);
+    return v < 0.25f ? near : __builtin_fmaf(-a, a, 1.f);
 }
 struct Gates {
     float a;      // what the state keeps

@@ -25,7 +25,7 @@ template <typename E, int V> __global__ __launch_bounds__(kStepThreads) void rec
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const Gates g = gates_of(r[v], i[v], decay_rate(d[v], sharpness));
-        h[v] = __builtin_fmaf(g.a, h[v], added(g, x[v]));
+        h[v] = __builtin_fmaf(g.a, h[v], added(g, x[v])), pin(h[v]);
     }
     state_row_store<V>(states, b, channels, c, h);
     row_store<E, V>(y, b, y_stride, c, h);
@@ -96,7 +96,7 @@ template <typename E, int V> __global__ __launch_bounds__(64) void rec_step_tree
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Gates g = gates_of(rv[v], iv[v], rate[v]);
-                h[v] = __builtin_fmaf(g.a, h[v], added(g, xv[v]));
+                h[v] = __builtin_fmaf(g.a, h[v], added(g, xv[v])), pin(h[v]);
                 lds[(k % nodes * 64 + l) * V + v] = h[v];
             }
             if (c_ok) {

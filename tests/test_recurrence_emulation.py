@@ -27,7 +27,11 @@ def emu(tmp_path_factory):
     for name in ("rec_scan", "rec_step"):
         _convert(os.path.join(CSRC, name + ".hip"), os.path.join(d, name + ".cpp"))
         srcs.append(os.path.join(d, name + ".cpp"))
-    _convert(os.path.join(CSRC, "rec_common.h"), os.path.join(d, "rec_common.h"))
+    common = open(os.path.join(CSRC, "rec_common.h")).read()
+    pinned = 'asm volatile("" : "+v"(v));'  # a hint for the compiler: nothing to emulate
+    assert common.count(pinned) == 1
+    open(os.path.join(d, "common.h"), "w").write(common.replace(pinned, ""))
+    _convert(os.path.join(d, "common.h"), os.path.join(d, "rec_common.h"))
     flags = ["-std=c++17", "-O2", "-fno-strict-aliasing", "-ffp-contract=off", "-Wno-psabi", "-Wno-unused-value", "-D__popcll=__builtin_popcountll",
              "-I", d, "-I", HERE, "-I", EMU, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     procs = [subprocess.Popen([CLANG, *flags, "-c", s, "-o", os.path.join(d, f"{i}.o")], stderr=subprocess.PIPE, text=True)
