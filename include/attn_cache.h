@@ -230,9 +230,13 @@ int attn_draft_tree(int32_t batch, int64_t total_tokens, int32_t words, const in
                     const int32_t *cu_seqlens, const int32_t *cached_lens, int32_t window, int32_t sinks,
                     int32_t *positions, int32_t *seen, void *hip_stream);
 
+/* As attn_workspace_bytes, for attn_attend_tree. */
+int attn_tree_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t max_new,
+                              size_t *bytes);
+
 /*
- * attn_attend for such a step, with the same arguments, workspace and results,
- * but that the query of new token i sees
+ * attn_attend for such a step, with the same arguments and results, but that the
+ * query of new token i sees
  *
  *   cached keys j < cached_lens[b] by its position p = positions[t]:
  *       window == 0  or  j > p - window  or  j < sinks

@@ -71,6 +71,8 @@ def load_library():
     lib.attn_attend.restype = ctypes.c_int
     lib.attn_attend.argtypes = [shape, i32, i64, i32, i32, vp, i64, vp, vp, vp, vp, vp, ctypes.c_float, i32, i32, i32, vp,
                                 i64, vp, vp, ctypes.c_size_t, vp]
+    lib.attn_tree_workspace_bytes.restype = ctypes.c_int
+    lib.attn_tree_workspace_bytes.argtypes = [shape, i32, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
     lib.attn_draft_tree.restype = ctypes.c_int
     lib.attn_draft_tree.argtypes = [i32, i64, i32, vp, vp, vp, i32, i32, vp, vp, vp]
     lib.attn_attend_tree.restype = ctypes.c_int

@@ -42,7 +42,7 @@ def build_prefix_cache(verbose: bool = False) -> str:
 
 
 ATTN_LIB_PATH = os.path.join(_PKG, "libattn_cache.so")
-ATTN_SOURCES = ["attn_api.hip", "attn_step.hip", "attn_tree.hip", "attn_attend.hip"]
+ATTN_SOURCES = ["attn_api.hip", "attn_step.hip", "attn_tree.hip", "attn_attend.hip", "attn_tree_attend.hip"]
 
 
 def build_attention(verbose: bool = False) -> str:

@@ -182,8 +182,7 @@ extern "C" int attn_rope_append(const attn_shape_t *shape, int64_t total_tokens,
                                        v_cache, static_cast<hipStream_t>(hip_stream)));
 }
 
-extern "C" int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t max_new,
-                                    size_t *bytes)
+static int attend_workspace(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t max_new, bool trees, size_t *bytes)
 {
     int rc = check_attend_shape(shape);
     if (rc == ATTN_OK)
@@ -192,8 +191,20 @@ extern "C" int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, in
         return rc;
     if (!bytes || max_new < 0)
         return fail(ATTN_ERR_INVALID_ARG, "bytes is NULL or max_new negative");
-    *bytes = attn_attend_workspace(*shape, batch, total_tokens, max_new);
+    *bytes = trees ? attn_attend_tree_workspace(*shape, batch, total_tokens, max_new) : attn_attend_workspace(*shape, batch, total_tokens, max_new);
     return ATTN_OK;
+}
+
+extern "C" int attn_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t max_new,
+                                    size_t *bytes)
+{
+    return attend_workspace(shape, batch, total_tokens, max_new, false, bytes);
+}
+
+extern "C" int attn_tree_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t max_new,
+                                         size_t *bytes)
+{
+    return attend_workspace(shape, batch, total_tokens, max_new, true, bytes);
 }
 
 static int attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks, int32_t max_blocks,
@@ -226,16 +237,21 @@ static int attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens
         return rc;
     if (!aligned16(k_cache) || !aligned16(v_cache))
         return fail(ATTN_ERR_MISALIGNED, "device pointers must be 16-byte aligned");
-    const size_t need = attn_attend_workspace(*shape, batch, total_tokens, max_new);
+    const bool is_tree = trees.words > 0;
+    const size_t need = is_tree ? attn_attend_tree_workspace(*shape, batch, total_tokens, max_new) : attn_attend_workspace(*shape, batch, total_tokens, max_new);
     if (need) {
         if (!workspace || workspace_bytes < need)
             return fail(ATTN_ERR_WORKSPACE_TOO_SMALL, "workspace is NULL or smaller than attn_workspace_bytes");
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
             return fail(ATTN_ERR_MISALIGNED, "workspace is not 256-byte aligned");
     }
+    if (is_tree)
+        return hip_status(launch_attn_attend_tree(*shape, batch, total_tokens, n_blocks, max_blocks, q, q_stride, k_cache, v_cache,
+                                                  table, cu_seqlens, cached_lens, scale, window, sinks, max_new, out, out_stride,
+                                                  lse, workspace, static_cast<hipStream_t>(hip_stream), trees));
     return hip_status(launch_attn_attend(*shape, batch, total_tokens, n_blocks, max_blocks, q, q_stride, k_cache, v_cache,
                                          table, cu_seqlens, cached_lens, scale, window, sinks, max_new, out, out_stride, lse,
-                                         workspace, static_cast<hipStream_t>(hip_stream), trees));
+                                         workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" int attn_attend(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks,

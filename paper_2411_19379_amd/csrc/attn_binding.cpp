@@ -174,7 +174,7 @@ PyObject *attend_with(PyObject *const *args, bool trees)
     if (want_lse < 0)
         throw python_error();
     size_t need = 0;
-    check(attn_workspace_bytes(&s, size32(batch, "batch"), T, max_new, &need));
+    check((trees ? attn_tree_workspace_bytes : attn_workspace_bytes)(&s, size32(batch, "batch"), T, max_new, &need));
     const at::Tensor out = more[4] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(more[4], "out");
     void *out_at = rows("out", out, {T, s.n_q_heads, s.head_dim}, type, device, &out_stride);
     at::Tensor lse, workspace;

@@ -492,6 +492,11 @@ hipError_t launch_attn_attend(const attn_shape_t &s, int batch, int64_t T, int n
                               const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
                               void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream,
                               const AttnTrees &trees = AttnTrees());
+size_t attn_attend_tree_workspace(const attn_shape_t &s, int batch, int64_t T, int max_new);
+hipError_t launch_attn_attend_tree(const attn_shape_t &s, int batch, int64_t T, int n_blocks, int max_blocks, const void *q,
+                                   int64_t q_stride, const void *k_cache, const void *v_cache, const int32_t *table,
+                                   const int32_t *cu, const int32_t *cached, float scale, int window, int sinks, int max_new,
+                                   void *out, int64_t out_stride, float *lse, void *workspace, hipStream_t stream, const AttnTrees &trees);
 constexpr int kMostTreeWords = 32;   // a tree has up to 1024 tokens
 constexpr int kCachesPerLaunch = 32; // their pointers travel in the kernel's arguments
 hipError_t launch_attn_draft_tree(int batch, int64_t T, int words, const int32_t *parents, const int32_t *cu, const int32_t *cached,

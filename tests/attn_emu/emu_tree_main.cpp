@@ -96,10 +96,10 @@ int main(int argc, char **argv)
             unsigned char *q = array<unsigned char>(T * row * esz), *k = array<unsigned char>(cache), *v = array<unsigned char>(cache);
             unsigned char *o = blank<unsigned char>(T * row * esz);
             float *lse = blank<float>((size_t)T * s.n_q_heads);
-            const size_t need = attn_attend_workspace(s, batch, T, max_new);
+            const size_t need = attn_attend_tree_workspace(s, batch, T, max_new);
             unsigned char *ws = blank<unsigned char>(need);
             memset(ws, 0xFF, need);  // NaN patterns
-            e = launch_attn_attend(s, batch, T, n_blocks, max_blocks, q, row, k, v, table, cu, cached, scale, window, sinks, max_new, o, row,
+            e = launch_attn_attend_tree(s, batch, T, n_blocks, max_blocks, q, row, k, v, table, cu, cached, scale, window, sinks, max_new, o, row,
                                    lse, ws, nullptr, trees);
             fwrite(o, 1, T * row * esz, out);
             fwrite(lse, 4, (size_t)T * s.n_q_heads, out);

@@ -24,8 +24,12 @@ def emu(tmp_path_factory):
         pytest.skip("no clang++ with bf16 vector support found")
     d = str(tmp_path_factory.mktemp("tree_emu"))
     srcs = [os.path.join(EMU, "emu_rt.cpp"), os.path.join(HERE, "emu_tree_main.cpp")]
-    for name in ("attn_tree", "attn_attend"):
-        _convert(os.path.join(CSRC, name + ".hip"), os.path.join(d, name + ".cpp"))
+    waits = 'asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");'
+    for name in ("attn_tree", "attn_attend", "attn_tree_attend"):
+        source = open(os.path.join(CSRC, name + ".hip")).read()
+        assert source.count(waits) == (name == "attn_tree_attend")
+        open(os.path.join(d, name + ".hip"), "w").write(source.replace(waits, "emu::memory_wait_but(N, __LINE__);"))
+        _convert(os.path.join(d, name + ".hip"), os.path.join(d, name + ".cpp"))
         srcs.append(os.path.join(d, name + ".cpp"))
     common = open(os.path.join(CSRC, "attn_common.h")).read()
     for asm, call in _COPIES:
@@ -34,7 +38,7 @@ def emu(tmp_path_factory):
     open(os.path.join(d, "common.h"), "w").write(common)
     _convert(os.path.join(d, "common.h"), os.path.join(d, "attn_common.h"))
     flags = ["-std=c++17", "-O2", "-fno-strict-aliasing", "-ffp-contract=off", "-Wno-psabi", "-Wno-unused-value", "-D__popcll=__builtin_popcountll",
-             "-DATTN_TARGET=emu::env_int(\"EMU_TARGET\")", "-I", d, "-I", HERE, "-I", EMU, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+             "-include", os.path.join(HERE, "tree_emu.h"), "-DATTN_TARGET=emu::env_int(\"EMU_TARGET\")", "-I", d, "-I", HERE, "-I", EMU, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     procs = [subprocess.Popen([CLANG, *flags, "-c", s, "-o", os.path.join(d, f"{i}.o")], stderr=subprocess.PIPE, text=True)
              for i, s in enumerate(srcs)]
     for p in procs:
