@@ -32,76 +32,78 @@ template <typename E, int V> __global__ __launch_bounds__(kStepThreads) void rec
 }
 
 // ---------------------------------------------------------------- trees
-// A wave per sequence and 64 V channels, token by token; the states of the last kNodes tokens stay in LDS for their children, older
-// ones are read back.  Inputs do not depend on the states and are requested kTreeAhead tokens ahead.
+// A wave per sequence and 64 channels, kTreeAhead tokens at a time, whose inputs are requested while those in front are worked on.  Their
+// gates, which are nearly all of the work and do not depend on states, are computed side by side; then the states, a product and
+// a sum each, those of the last kNodes tokens kept in LDS for their children (older ones are read back).  Memory latency bounds it:
+// 32 trees of 16 to 64 tokens of 4096 channels in bf16 23.5 us, of which the stores 6 and the gates 2 (two channels per thread and one
+// token at a time 26.8, four waves that share a batch's gates 34); one tree of 17 tokens 6.9 us (8.6 and 6.0).
 constexpr int kNodes = 64;
 constexpr int kTreeAhead = 8;
-template <typename E, int V> __global__ __launch_bounds__(64) void rec_step_tree_kernel(RecIo in, const float *decay, float sharpness, int channels, const float *states,
-                                                                                       const int32_t *cu, const int32_t *parents, int64_t T, void *y, int64_t y_stride,
-                                                                                       float *node_states, int nodes)
+template <typename E> __global__ __launch_bounds__(64) void rec_step_tree_kernel(RecIo in, const float *decay, float sharpness, int channels, const float *states, const int32_t *cu,
+                                                                                const int32_t *parents, int64_t T, void *y, int64_t y_stride, float *node_states, int nodes)
 {
     extern __shared__ __align__(16) unsigned char lds_raw[];
-    float *const lds = reinterpret_cast<float *>(lds_raw);  // [nodes][64][V]
+    float *const lds = reinterpret_cast<float *>(lds_raw);  // [nodes][64]
     const int l = threadIdx.x, b = blockIdx.y;
     const RecSeq s = rec_seq(cu, b, T);
-    const int own = (blockIdx.x * 64 + l) * V;
+    const int own = blockIdx.x * 64 + l;
     const bool c_ok = own < channels;
     const int c = c_ok ? own : 0;
     if (s.n == 0)
         return;
-    typedef RecRow<E, V> Row;
-    float root[V], rate[V], h[V];
-    state_row_load<V>(states, b, channels, c, root);
-    state_row_load<V>(decay, 0, channels, c, rate);
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        rate[v] = decay_rate(rate[v], sharpness), h[v] = 0.f;
+    typedef RecRow<E, 1> Row;
     typename Row::Raw x[kTreeAhead], r[kTreeAhead], i[kTreeAhead];
-    int parent[kTreeAhead];
-    auto request = [&](int u, int k) __attribute__((always_inline)) {
-        const int64_t t = s.start + (int64_t)(k < s.n ? k : s.n - 1);
-        x[u] = row_load<E, V>(in.x, t, in.x_stride, c);
-        r[u] = row_load<E, V>(in.r, t, in.r_stride, c);
-        i[u] = row_load<E, V>(in.i, t, in.i_stride, c);
-        parent[u] = parents[t];
-    };
-#pragma unroll
-    for (int u = 0; u < kTreeAhead; ++u)
-        request(u, u);
-    for (int k0 = 0; k0 < s.n; k0 += kTreeAhead) {
+    int parent = 0;  // of token l of the present and the next ones
+    auto request = [&](int k0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kTreeAhead; ++u) {
-            const int k = k0 + u;
+            const int64_t t = s.start + (int64_t)(k0 + u < s.n ? k0 + u : s.n - 1);
+            x[u] = row_load<E, 1>(in.x, t, in.x_stride, c);
+            r[u] = row_load<E, 1>(in.r, t, in.r_stride, c);
+            i[u] = row_load<E, 1>(in.i, t, in.i_stride, c);
+        }
+        if (k0 % 64 == 0)
+            parent = parents[s.start + (int64_t)(k0 + l < s.n ? k0 + l : s.n - 1)];
+    };
+    const float rate = decay_rate(decay[c], sharpness), root = states[(int64_t)b * channels + c];
+    float h = 0.f;
+    request(0);
+    for (int k0 = 0; k0 < s.n; k0 += kTreeAhead) {
+        float kept[kTreeAhead], add[kTreeAhead];
+        int from[kTreeAhead];
+#pragma unroll
+        for (int u = 0; u < kTreeAhead; ++u) {
+            float xv, rv, iv;
+            Row::unpack(x[u], &xv);
+            Row::unpack(r[u], &rv);
+            Row::unpack(i[u], &iv);
+            const Gates g = gates_of(rv, iv, rate);
+            kept[u] = g.a, add[u] = added(g, xv);
+            from[u] = __builtin_amdgcn_readlane(parent, (k0 + u) % 64);
+        }
+        if (k0 + kTreeAhead < s.n)
+            request(k0 + kTreeAhead);
+#pragma unroll
+        for (int u = 0; u < kTreeAhead; ++u) {
+            const int k = k0 + u, p = from[u];
             if (k >= s.n)
                 break;
-            float xv[V], rv[V], iv[V];
-            Row::unpack(x[u], xv);
-            Row::unpack(r[u], rv);
-            Row::unpack(i[u], iv);
-            const int p = __builtin_amdgcn_readfirstlane(parent[u]);
-            request(u, k + kTreeAhead);
-            if (p < 0 || p >= k) {
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-                    h[v] = root[v];
-            } else if (p != k - 1) {
-                if (k - p <= nodes) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        h[v] = lds[(p % nodes * 64 + l) * V + v];
-                } else if (c_ok) {
-                    state_row_load<V>(node_states, s.start + (int64_t)p, channels, c, h);
+            if (p != k - 1 || k == 0) {
+                h = root;
+                if (p >= 0 && p < k) {
+                    if (k - p <= nodes) {
+                        h = lds[p % nodes * 64 + l];
+                    } else {
+                        h = node_states[(s.start + (int64_t)p) * channels + c];
+                        pin(h);  // waited for here: behind the branch every token would wait for all loads and stores on their way
+                    }
                 }
             }
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Gates g = gates_of(rv[v], iv[v], rate[v]);
-                h[v] = __builtin_fmaf(g.a, h[v], added(g, xv[v])), pin(h[v]);
-                lds[(k % nodes * 64 + l) * V + v] = h[v];
-            }
+            h = __builtin_fmaf(kept[u], h, add[u]), pin(h);
+            lds[k % nodes * 64 + l] = h;
             if (c_ok) {
-                row_store<E, V>(y, s.start + (int64_t)k, y_stride, own, h);
-                state_row_store<V>(node_states, s.start + (int64_t)k, channels, own, h);
+                row_store<E, 1>(y, s.start + (int64_t)k, y_stride, own, &h);
+                node_states[(s.start + (int64_t)k) * channels + own] = h;
             }
         }
     }
@@ -129,12 +131,12 @@ template <typename E, int V> hipError_t step(const rec_shape_t &s, int batch, co
                        s.channels, states, y, y_stride);
     return hipGetLastError();
 }
-template <typename E, int V> hipError_t step_tree(const rec_shape_t &s, int batch, int64_t T, const RecIo &in, const float *decay, const float *states, const int32_t *cu,
-                                                  const int32_t *parents, void *y, int64_t y_stride, float *node_states, hipStream_t stream)
+template <typename E> hipError_t step_tree(const rec_shape_t &s, int batch, int64_t T, const RecIo &in, const float *decay, const float *states, const int32_t *cu,
+                                           const int32_t *parents, void *y, int64_t y_stride, float *node_states, hipStream_t stream)
 {
     const int nodes = T < kNodes ? (int)T : kNodes;
-    hipLaunchKernelGGL((rec_step_tree_kernel<E, V>), dim3((unsigned)((s.channels + 64 * V - 1) / (64 * V)), (unsigned)batch), dim3(64), (size_t)nodes * 64 * V * sizeof(float),
-                       stream, in, decay, s.sharpness, s.channels, states, cu, parents, T, y, y_stride, node_states, nodes);
+    hipLaunchKernelGGL((rec_step_tree_kernel<E>), dim3((unsigned)((s.channels + 63) / 64), (unsigned)batch), dim3(64), (size_t)nodes * 64 * sizeof(float), stream, in, decay,
+                       s.sharpness, s.channels, states, cu, parents, T, y, y_stride, node_states, nodes);
     return hipGetLastError();
 }
 
@@ -160,15 +162,11 @@ hipError_t launch_rec_step(const rec_shape_t &s, int batch, const RecIo &in, con
 hipError_t launch_rec_step_tree(const rec_shape_t &s, int batch, int64_t T, const RecIo &in, const float *decay, const float *states, const int32_t *cu,
                                 const int32_t *parents, void *y, int64_t y_stride, float *node_states, hipStream_t stream)
 {
-    const bool two = two_channels(s, in, y, y_stride, decay, states) && pairs(node_states, 0, 4);
     if (s.io_dtype == REC_DT_F32)
-        return two ? step_tree<RecF32, 2>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream)
-                   : step_tree<RecF32, 1>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
+        return step_tree<RecF32>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
     if (s.io_dtype == REC_DT_BF16)
-        return two ? step_tree<RecBf16, 2>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream)
-                   : step_tree<RecBf16, 1>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
-    return two ? step_tree<RecF16, 2>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream)
-               : step_tree<RecF16, 1>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
+        return step_tree<RecBf16>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
+    return step_tree<RecF16>(s, batch, T, in, decay, states, cu, parents, y, y_stride, node_states, stream);
 }
 
 hipError_t launch_rec_keep(int channels, int batch, int64_t T, float *states, const float *node_states, const int32_t *cu, const int32_t *path, const int32_t *counts,
