@@ -16,7 +16,7 @@
  *   rec_scan         packed sequences from initial states, states at chosen tokens
  *   rec_scan_grads   its backward pass
  *   rec_step         one token of every sequence, the states in place
- *   rec_step_tree    trees of drafted tokens (attn_cache.h), each token from its
+ *   rec_step_tree    trees of drafted tokens (attn_tree.h), each token from its
  *                    parent's state
  *   rec_keep_states  the state behind the last token that was kept
  *
@@ -92,8 +92,9 @@ int rec_workspace_bytes(const rec_shape_t *shape, int32_t batch, int64_t total_t
  *   saved         [ceil(total_tokens / REC_SAVED_EVERY), channels]  fp32 device,
  *                 out, or NULL: what rec_scan_grads takes
  *
- * init_states may be final_states.  Results do not depend on the timing of the
- * GPU.
+ * init_states may be final_states, and y may be x, r or i with its stride, as
+ * in rec_step and rec_step_tree; apart from that nothing that is written
+ * overlaps anything else.  Results do not depend on the timing of the GPU.
  */
 int rec_scan(const rec_shape_t *shape, int32_t batch, int64_t total_tokens,
              const void *x, int64_t x_stride, const void *r, int64_t r_stride, const void *i, int64_t i_stride,

@@ -1,4 +1,4 @@
-"""Binding of the attention layers' operators (`include/attn_cache.h`): argument marshalling only.
+"""Binding of the attention layers' operators (`include/attn_cache.h`, `include/attn_tree.h`): argument marshalling only.
 
     step = assign_blocks(block_size, total_tokens, cu_seqlens, cached_lens, table, free_blocks, n_free)   # once per step
     q = rope_append(q, k, v, step.positions, step.slots, rotary, k_cache, v_cache, copies=step.copies)    # once per layer

@@ -1,9 +1,9 @@
-// CPython binding of the attention operators over their C ABI (include/attn_cache.h): checks of tensors, outputs and workspace
+// CPython binding of the attention operators over their C ABI (include/attn_cache.h, include/attn_tree.h): checks of tensors, outputs and workspace
 // from torch's allocator, the current stream.  A decode step of a layer is a few microseconds of GPU work, and the same steps
 // written in Python with ctypes took longer than that (append 10.7 us and attention 10.0 us per call in front of the launches).
 #include "torch_binding.h"
 
-#include "attn_cache.h"
+#include "attn_tree.h"
 
 namespace {
 

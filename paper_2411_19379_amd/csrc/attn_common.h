@@ -2,7 +2,7 @@
 // query sees, the cache's rows.
 #pragma once
 
-#include "attn_cache.h"
+#include "attn_tree.h"
 #include "mfma_utils.h"
 
 namespace {

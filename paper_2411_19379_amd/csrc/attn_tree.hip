@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kDraftThreads) void attn_draft_tree_kernel(int batc
 // v_0 is the sequence's first token, v_(k+1) the first child of v_k that is the token chosen behind v_k.  A wave per sequence, a token
 // per lane and 64 at a time: children come behind their parents, so one walk over the tokens finds the branch.  One workgroup for the
 // batch, since the blocks that are given back go to the free list in the order of the sequences; a wave has the tokens of up
-// to kAcceptAtOnce sequences on their way at once.  Latency bounds it: a launch, four trips to memory and two barriers; one tree 4 us,
+// to kAcceptAtOnce sequences on their way at once.  Latency bounds it: a launch, four trips to memory and two barriers; one tree 4.5 us,
 // 64 trees of 16 to 64 tokens 12 us (walking four sequences side by side, with the blocks kept in registers, 11.7).
 constexpr int kAcceptThreads = 1024;
 constexpr int kAcceptWaves = kAcceptThreads / 64;

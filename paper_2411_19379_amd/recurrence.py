@@ -25,6 +25,7 @@ _lib = None
 
 REC_DT_F32, REC_DT_BF16, REC_DT_F16 = 0, 1, 2
 REC_SAVED_EVERY = 8
+REC_MOST_STRIDE = 1 << 22  # elements between tokens
 
 _STATUS = {0: "REC_OK", -1: "REC_ERR_INVALID_ARG", -4: "REC_ERR_UNSUPPORTED_SHAPE", -5: "REC_ERR_WORKSPACE_TOO_SMALL",
            -6: "REC_ERR_MISALIGNED", -7: "REC_ERR_HIP"}
@@ -124,11 +125,11 @@ class _Differentiable(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy, d_final):
         x, r, i, decay, init_states, cu_seqlens, saved = ctx.saved_tensors
-        _not_captured()
+        _not_captured(x)
         if dy is None and d_final is None:
             return (None,) * 7
         if dy is not None and not _in_rows(dy):
-            dy = dy.contiguous()  # an expanded gradient, as a sum's is
+            dy = dy.contiguous()  # an expanded gradient, as a sum's is, or rows further apart than the kernels take
         if d_final is not None:
             d_final = d_final.contiguous()
         grads = _native().scan_grads(x, r, i, decay, cu_seqlens, ctx.sharpness, init_states, saved, dy, d_final, init_states is not None)
@@ -136,11 +137,11 @@ class _Differentiable(torch.autograd.Function):
 
 
 def _in_rows(t) -> bool:
-    return t.stride(1) == 1 and t.stride(0) >= t.shape[1] or t.is_contiguous()
+    return t.stride(1) == 1 and t.shape[1] <= t.stride(0) <= REC_MOST_STRIDE or t.is_contiguous()
 
 
-def _not_captured():
-    if torch.cuda.is_current_stream_capturing():
+def _not_captured(x):
+    if x.is_cuda and torch.cuda.is_current_stream_capturing():
         raise RuntimeError("a graph of gradients is not captured: capture gated_scan under torch.no_grad() and gated_scan_grads")
 
 
@@ -154,7 +155,7 @@ def gated_scan(x, r, i, decay, cu_seqlens, *, sharpness: float = 8.0, init_state
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, r, i, decay, init_states)):
         if ckpt is not None or out is not None:
             raise ValueError("ckpt and out are not differentiable: call under torch.no_grad(), or detach")
-        _not_captured()
+        _not_captured(x)
         return GatedScan(*_Differentiable.apply(x, r, i, decay, init_states, cu_seqlens, sharpness), None)
     if out is not None and out.requires_grad and torch.is_grad_enabled():
         raise ValueError("out requires grad: call under torch.no_grad(), or detach")

@@ -276,6 +276,50 @@ def test_two_calls_at_once():
         assert all(torch.equal(u, v) for u, v in zip(b, grads))
 
 
+@pytest.mark.parametrize("C,dtype", [(70, "bf16"), (128, "f32"), (33, "f16")])
+def test_in_place(C, dtype):
+    """y in the place of an input, and the final states in that of the initial ones."""
+    p = rh.make(9, C, dtype, [400, 0, 3, 130])
+    x, r, i, decay, cu, init = _on_gpu(p)
+    inside = slice(int(p.cu[0]), int(p.cu[-1]))
+    states = torch.randn(p.T, C, device=DEV)
+    parents = _ints(np.concatenate([np.full(int(p.cu[0]), -1)] + [np.arange(n) // 2 - 1 for n in p.lens] + [np.full(p.T - int(p.cu[-1]), -1)]))
+    for at in range(3):
+        def arguments():
+            args = [t.clone() for t in (x, r, i)]
+            return args, args[at]
+        args, out = arguments()
+        want = rec.gated_scan(*args, decay, cu, init_states=init)
+        got = rec.gated_scan(*args, decay, cu, init_states=init, out=out)
+        assert got.y is out and torch.equal(out[inside], want.y[inside]) and torch.equal(got.final, want.final)
+        args, out = arguments()
+        y, nodes = rec.gated_step_tree(*args, decay, init, cu, parents)
+        again, same = rec.gated_step_tree(*args, decay, init, cu, parents, out=out)
+        assert torch.equal(again[inside], y[inside]) and torch.equal(same[inside], nodes[inside])
+        args, out = arguments()
+        one, two = states.clone(), states.clone()
+        y = rec.gated_step(*args, decay, one)
+        assert torch.equal(rec.gated_step(*args, decay, two, out=out), y) and torch.equal(one, two)
+    both, y, shape = init.clone(), torch.empty_like(x), rec.RecShape(C, rh.CODE[dtype], 8.0)
+    ws = torch.empty(rec.rec_workspace_bytes(shape, len(p.lens), p.T), dtype=torch.uint8, device=DEV)
+    want = rec.gated_scan(x, r, i, decay, cu, init_states=init)
+    rows = [v for t in (x, r, i) for v in (t.data_ptr(), C)]
+    rc = rec.load_library().rec_scan(shape, len(p.lens), p.T, *rows, decay.data_ptr(), cu.data_ptr(), both.data_ptr(), None, 0, y.data_ptr(), C,
+                                     both.data_ptr(), None, None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    assert rc == 0 and torch.equal(both, want.final) and torch.equal(y[inside], want.y[inside])
+
+
+def test_gradients_that_are_far_apart_or_expanded():
+    p = rh.make(6, 40, "bf16", [3])
+    x, r, i, decay, cu, _ = _on_gpu(p)
+    want = rec.gated_scan_grads(torch.ones_like(x), None, x, r, i, decay, cu)
+    wide = torch.ones(p.T, rec.REC_MOST_STRIDE + 8, device=DEV, dtype=x.dtype)[:, :p.C]
+    for dy in (wide, torch.ones(1, 1, device=DEV, dtype=x.dtype).expand(p.T, p.C)):
+        leaf = x.clone().requires_grad_()
+        rec.gated_scan(leaf, r, i, decay, cu).y.backward(dy)
+        assert torch.equal(leaf.grad, want.x)
+
+
 def test_no_tokens():
     x, decay, states = torch.zeros(0, 6, device=DEV), torch.zeros(6, device=DEV), torch.randn(2, 6, device=DEV)
     cu = _ints([0, 0, 0])
