@@ -13,10 +13,20 @@
 // last such state, the maps of the groups behind it and those of the chunks of its own group, in this order, so that sums do not
 // depend on timing.  What is published is one 64-bit word per channel, which holds a pattern that no result has until it is there:
 // no other memory has to be ordered by it.
+//
+// Memory bounds long batches, and beside it the wait for the state in front, 30 to 50 us of the first: a prompt of 32768 tokens of 4096
+// channels in bf16 265 us, 1.09 GB at 4.1 TB/s where copies reach 4.9, vector units busy 53 % of the time;  13877 tokens of 2560
+// channels forwards 73 us, 3.8 TB/s, backwards 139 us, 0.55 GB at 3.9 TB/s, vector units 40 %.  (One level of published maps and chunks
+// of 64 tokens: 293, 85 and 219 us.)  Short ones are latency: a launch that empties the words, a ticket, lengths, inputs, two
+// or three waits for words, 11 us for 800 tokens of 256 channels.
 #include <cmath>
 #include <type_traits>
 
 #include "rec_common.h"
+
+#ifndef REC_FEW_WORKGROUPS  // tests with small batches choose others
+#define REC_FEW_WORKGROUPS 128
+#endif
 
 namespace {
 
@@ -680,11 +690,15 @@ hipError_t prepare(const rec_shape_t &s, const Workspace &w, const Look &look, c
 }
 
 bool pairs(const void *p, int64_t stride, int bytes) { return reinterpret_cast<uintptr_t>(p) % (2 * bytes) == 0 && stride % 2 == 0; }
-// Two channels per lane: half of the loads, where rows allow it.
-bool two_channels(const rec_shape_t &s, const RecIo &in)
+// Two channels per lane, half of the loads, where rows allow it and more than REC_FEW_WORKGROUPS are left: with one there are twice as
+// many, which 256 compute units can all run at once (us, one channel and two; bf16, 1000 channels, scan of 1600 tokens, 104 workgroups,
+// 14.0 and 15.8, of 3200, 200, 19.6 and 17.8, of 32768 tokens of 4096 channels 293 and 264; gradients of 800 tokens, 104, 16.7 and
+// 18.5, of 1600, 200, 23.0 and 22.1, of 12800 tokens of 2560 channels 170 and 151).
+bool two_channels(const rec_shape_t &s, const RecIo &in, int64_t T, int chunk)
 {
     const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
-    return s.channels % 2 == 0 && pairs(in.x, in.x_stride, e) && pairs(in.r, in.r_stride, e) && pairs(in.i, in.i_stride, e);
+    return s.channels % 2 == 0 && (s.channels + 127) / 128 * ((T + chunk - 1) / chunk) > REC_FEW_WORKGROUPS && pairs(in.x, in.x_stride, e) && pairs(in.r, in.r_stride, e) &&
+           pairs(in.i, in.i_stride, e);
 }
 
 template <typename K> hipError_t lds_limit(K kernel, size_t lds)
@@ -733,7 +747,6 @@ hipError_t copy_states(float *to, const float *from, int64_t n, hipStream_t stre
 
 }  // namespace
 
-// A lane with one channel has the smaller chunks, and with them the larger workspace.
 size_t rec_scan_workspace(const rec_shape_t &s, int batch, int64_t T, int grads)
 {
     if (T == 0 || batch == 0)
@@ -751,7 +764,7 @@ hipError_t launch_rec_scan(const rec_shape_t &s, const RecScan &a, void *workspa
     }
     unsigned char *const at = static_cast<unsigned char *>(workspace);
     const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
-    const bool two = two_channels(s, a.in) && pairs(a.init, 0, 4) && (!a.y || pairs(a.y, a.y_stride, e)) && pairs(a.final_states, 0, 4) && pairs(a.ckpt_states, 0, 4) &&
+    const bool two = two_channels(s, a.in, a.T, Place<2, kScanTokens>::kChunk) && pairs(a.init, 0, 4) && (!a.y || pairs(a.y, a.y_stride, e)) && pairs(a.final_states, 0, 4) && pairs(a.ckpt_states, 0, 4) &&
                      pairs(a.saved, 0, 4);
     if (s.io_dtype == REC_DT_F32)
         return two ? scan<RecF32, 2>(s, a, at, stream) : scan<RecF32, 1>(s, a, at, stream);
@@ -769,10 +782,11 @@ hipError_t launch_rec_grads(const rec_shape_t &s, const RecGrads &given, void *w
     }
     unsigned char *const at = static_cast<unsigned char *>(workspace);
     const bool again = !a.saved;
-    const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
-    const bool two = two_channels(s, a.in) && pairs(a.init, 0, 4) && (!a.dy || pairs(a.dy, a.dy_stride, e)) && pairs(a.saved, 0, 4) && pairs(a.d_final, 0, 4) &&
-                     pairs(a.dx, 0, e) && pairs(a.dr, 0, e) && pairs(a.di, 0, e) && pairs(a.d_init, 0, 4);
-    const Workspace w(s.channels, a.T, two ? Place<2, kGradsTokens>::kChunk : Place<1, kGradsTokens>::kChunk, again ? 2 : 1);
+    // fp32: rows of one channel per lane are 256 bytes already (12800 tokens of 2560 channels 209 us, two channels 232)
+    const bool two = s.io_dtype != REC_DT_F32 && two_channels(s, a.in, a.T, Place<2, kGradsTokens>::kChunk) && pairs(a.init, 0, 4) &&
+                     (!a.dy || pairs(a.dy, a.dy_stride, 2)) && pairs(a.saved, 0, 4) && pairs(a.d_final, 0, 4) && pairs(a.dx, 0, 2) && pairs(a.dr, 0, 2) &&
+                     pairs(a.di, 0, 2) && pairs(a.d_init, 0, 4);
+    const Workspace w(s.channels, a.T, Place<1, kGradsTokens>::kChunk, again ? 2 : 1);
     if (again) {
         // its maps lie in front of what it saves
         const size_t maps = Workspace(s.channels, a.T, Place<1, kScanTokens>::kChunk, 0).bytes;
@@ -785,7 +799,7 @@ hipError_t launch_rec_grads(const rec_shape_t &s, const RecGrads &given, void *w
             return e;
     }
     if (s.io_dtype == REC_DT_F32)
-        return two ? grads<RecF32, 2>(s, a, w, at, stream) : grads<RecF32, 1>(s, a, w, at, stream);
+        return grads<RecF32, 1>(s, a, w, at, stream);
     if (s.io_dtype == REC_DT_BF16)
         return two ? grads<RecBf16, 2>(s, a, w, at, stream) : grads<RecBf16, 1>(s, a, w, at, stream);
     return two ? grads<RecF16, 2>(s, a, w, at, stream) : grads<RecF16, 1>(s, a, w, at, stream);

@@ -39,7 +39,8 @@ def _numpy(*all_):
 
 SIZES = dict(rh.CASES)
 SIZES.update(long=(192, "bf16", [5000, 1], {}), wide=(2560, "bf16", [300, 129, 0, 64], {}), wide_odd=(1001, "f16", [500, 70], {}),
-             many=(128, "f32", [37] * 60 + [0] * 5, dict(init=False)))
+             many=(128, "f32", [37] * 60 + [0] * 5, dict(init=False)), two=(2560, "bf16", [900, 300, 0, 64], {}), two_f32=(2048, "f32", [1300], {}),
+             two_f16=(1000, "f16", [2500, 3], dict(init=False)))
 
 
 @pytest.mark.parametrize("apart", [True, False])
@@ -274,6 +275,20 @@ def test_two_calls_at_once():
     for a, b in outs:
         assert torch.equal(a.y, want.y) and torch.equal(a.final, want.final)
         assert all(torch.equal(u, v) for u, v in zip(b, grads))
+
+
+@pytest.mark.parametrize("name", ["two", "two_f32", "two_f16", "long"])
+def test_unaligned_rows_have_the_same_results(name):
+    C, dtype, lens, more = SIZES[name]
+    p = rh.make(12, C, dtype, lens, **more)
+    x, r, i, decay, cu, init = _on_gpu(p)
+    inside = slice(int(p.cu[0]), int(p.cu[-1]))
+    moved = torch.empty(p.T * C + 1, dtype=x.dtype, device=DEV)[1:].view(p.T, C).copy_(x)
+    a, b = (rec.gated_scan(t, r, i, decay, cu, init_states=init) for t in (x, moved))
+    assert torch.equal(a.y[inside], b.y[inside]) and torch.equal(a.final, b.final)
+    dy = p.dy.to(DEV)
+    for a, b in zip(*(rec.gated_scan_grads(dy, None, t, r, i, decay, cu, init_states=init) for t in (x, moved))):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("C,dtype", [(70, "bf16"), (128, "f32"), (33, "f16")])

@@ -18,11 +18,10 @@ from test_kernel_emulation import CLANG, CSRC, EMU, ROOT, _convert
 HERE = os.path.join(ROOT, "tests", "rec_emu")
 
 
-@pytest.fixture(scope="session")
-def emu(tmp_path_factory):
+def _build(d, few):
+    """The emulated kernels, two channels per lane where more than `few` workgroups are left."""
     if not os.path.exists(CLANG):
         pytest.skip("no clang++ with bf16 vector support found")
-    d = str(tmp_path_factory.mktemp("rec_emu"))
     srcs = [os.path.join(EMU, "emu_rt.cpp"), os.path.join(HERE, "emu_rec_main.cpp")]
     for name in ("rec_scan", "rec_step"):
         _convert(os.path.join(CSRC, name + ".hip"), os.path.join(d, name + ".cpp"))
@@ -32,7 +31,7 @@ def emu(tmp_path_factory):
     assert common.count(pinned) == 1
     open(os.path.join(d, "common.h"), "w").write(common.replace(pinned, ""))
     _convert(os.path.join(d, "common.h"), os.path.join(d, "rec_common.h"))
-    flags = ["-std=c++17", "-O2", "-fno-strict-aliasing", "-ffp-contract=off", "-Wno-psabi", "-Wno-unused-value", "-D__popcll=__builtin_popcountll",
+    flags = [f"-DREC_FEW_WORKGROUPS={few}", "-std=c++17", "-O2", "-fno-strict-aliasing", "-ffp-contract=off", "-Wno-psabi", "-Wno-unused-value", "-D__popcll=__builtin_popcountll",
              "-I", d, "-I", HERE, "-I", EMU, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     procs = [subprocess.Popen([CLANG, *flags, "-c", s, "-o", os.path.join(d, f"{i}.o")], stderr=subprocess.PIPE, text=True)
              for i, s in enumerate(srcs)]
@@ -42,6 +41,16 @@ def emu(tmp_path_factory):
     exe = os.path.join(d, "emu_rec_main")
     subprocess.run([CLANG, *[os.path.join(d, f"{i}.o") for i in range(len(srcs))], "-o", exe], check=True)
     return exe
+
+
+@pytest.fixture(scope="session")
+def emu(tmp_path_factory):
+    return _build(str(tmp_path_factory.mktemp("rec_emu")), 0)
+
+
+@pytest.fixture(scope="session")
+def emu_few(tmp_path_factory):
+    return _build(str(tmp_path_factory.mktemp("rec_emu_few")), 1 << 20)
 
 
 ORDERS = [(1, "start"), (5, "end")]
@@ -124,6 +133,15 @@ def test_scan_not_finite_stays_in_its_sequence(emu, tmp_path, where):
         h, want_final = rh.reference(p)
         y, final, _, _ = _scan(emu, tmp_path, p)
         assert np.array_equal(np.isfinite(y), np.isfinite(h)) and np.array_equal(np.isfinite(final), np.isfinite(want_final))
+
+
+@pytest.mark.parametrize("name", ["chunks", "groups"])
+def test_one_channel_per_lane_is_two(emu, emu_few, tmp_path, name):
+    C, dtype, lens, more = rh.CASES[name]
+    p = rh.make(8, C, dtype, lens, **more)
+    for call in (lambda exe: _scan(exe, tmp_path, p, [0, p.T // 2]), lambda exe: _grads(exe, tmp_path, p)):
+        for a, b in zip(call(emu), call(emu_few)):
+            assert np.array_equal(a, b, equal_nan=True)
 
 
 def _grads(exe, tmp_path, p, dy=True, d_final=True, init=True, gap=0, order=0, side="end"):
