@@ -33,13 +33,14 @@ __global__ __launch_bounds__(kDraftThreads) void attn_draft_tree_kernel(int batc
     const int tid = threadIdx.x;
     if ((int)blockIdx.x == batch) {  // tokens of no sequence
         const int first = cu[0] > 0 ? cu[0] : 0, last = cu[batch] < 0 ? 0 : cu[batch];
-        for (int64_t t = tid; t < T; t += kDraftThreads) {
-            if (t >= first && t < last)
-                continue;
-            positions[t] = 0;
-            for (int w = 0; w < words; ++w)
-                seen[t * words + w] = 0;
-        }
+        auto clear = [&](int64_t from, int64_t to) __attribute__((always_inline)) {
+            for (int64_t t = from + tid; t < to; t += kDraftThreads)
+                positions[t] = 0;
+            for (int64_t k = from * words + tid; k < to * words; k += kDraftThreads)
+                seen[k] = 0;
+        };
+        clear(0, first < T ? first : T);
+        clear(last < first ? first : last, T);
         return;
     }
     const TreeSeq s = tree_seq(cu, cached, blockIdx.x, T);

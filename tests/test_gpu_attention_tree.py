@@ -255,6 +255,27 @@ def test_rows_of_no_sequence_stay_as_they_are():
     assert np.array_equal(out[:p.T].cpu().double().numpy(), _attend(p)[0])
 
 
+@pytest.mark.parametrize("new", [[3, 2], [17, 40], [300]])
+def test_caches_beyond_32_bits(new):
+    """Blocks whose elements lie behind 2^32: the same results, bit for bit, as in a small cache."""
+    p = th.make(31, 8, 2, 128, 16, "bf16", new, [100 + 7 * b for b in range(len(new))], max_new=max(new))
+    small = [p.k_cache.to(DEV), p.v_cache.to(DEV)]
+    n, blocks = small[0].shape[0], (1 << 32) // (2 * 16 * 128) + 50
+    caches = [torch.empty(blocks, 2, 16, 128, dtype=torch.bfloat16, device=DEV) for _ in small]
+    for c, s in zip(caches, small):
+        c[blocks - n:] = s
+    table = np.asarray(p.table)
+    args = (_ints(p.cu), _ints(p.cached), _ints(p.positions), _ints(p.bits))
+    far = _ints(np.where(table >= 0, table + blocks - n, table))
+    a, b = (attn.attend_tree(p.q.to(DEV), *c, t, *args, scale=p.scale, max_new=p.max_new) for c, t in ((small, _ints(table)), (caches, far)))
+    assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    path = _ints(np.concatenate([np.minimum(2 * np.arange(m), m - 1) if m < 3 else np.concatenate([np.arange(0, m, 2), np.full(m // 2, -1)]) for m in new]))
+    for c, t in ((small, _ints(table)), (caches, far)):
+        attn.keep_path(c, t, args[0], args[1], path)
+    bits = lambda t: t.view(torch.int16)  # (rows that hold no key are NaN)
+    assert all(torch.equal(bits(c[blocks - n:]), bits(s)) for c, s in zip(caches, small))
+
+
 def test_no_tokens():
     none, cu, one = _ints([]), _ints([0, 0]), _ints([3])
     tree = attn.draft_tree(none, cu, one, 5)

@@ -335,6 +335,39 @@ def test_gradients_that_are_far_apart_or_expanded():
         assert torch.equal(leaf.grad, want.x)
 
 
+def test_tensors_beyond_32_bits():
+    """2^31 elements and some rows: the last sequences as in a batch of their own."""
+    C, n = 4096, 300
+    T = (1 << 31) // C + 200
+    g = torch.Generator(DEV).manual_seed(4)
+    tail = [torch.randn(n, C, device=DEV, generator=g).bfloat16() for _ in range(3)]
+    x = torch.zeros(T, C, dtype=torch.bfloat16, device=DEV)
+    r, i = torch.zeros_like(x), torch.zeros_like(x)
+    for whole, part in zip((x, r, i), tail):
+        whole[T - n:] = part
+    decay, init = torch.randn(C, device=DEV, generator=g), torch.randn(3, C, device=DEV, generator=g)
+    cu, own = _ints([0, T - n, T - 100, T]), _ints([0, n - 100, n])
+    want, got = rec.gated_scan(*tail, decay, own, init_states=init[1:], ckpt=_ints([n - 2])), rec.gated_scan(x, r, i, decay, cu, init_states=init, ckpt=_ints([T - 2]))
+    # Chunks fall elsewhere, so maps are composed in another order.  A token's step costs a state at most 32 half-steps of 2^-24 of the
+    # largest one: the sum's 1, those of a (exponent, its argument's relative to |log a| a <= 1/e, the composed product) 11, and 10 of
+    # the added term, which is at most twice the largest state.  Both sides are that far off after at most n tokens.
+    apart = 2 * n * 32 * 2.0 ** -24
+    assert float((got.ckpt_states - want.ckpt_states).abs().max()) <= apart * float(want.y.float().abs().max())
+    assert float((got.final[1:] - want.final).abs().max()) <= apart * float(want.y.float().abs().max())
+    # a step of bf16 where that decides a rounding
+    assert float((got.y[T - n:].float() - want.y.float()).abs().max()) <= 2.0 ** -7 * float(want.y.float().abs().max())
+    parents = _ints(np.concatenate([np.full(T - n, -1), np.arange(n - 100) - 1, np.arange(100) // 2 - 1]))
+    y, nodes = rec.gated_step_tree(x, r, i, decay, init, cu, parents)
+    want_y, want_nodes = rec.gated_step_tree(*tail, decay, init[1:], own, parents[T - n:].contiguous())
+    assert torch.equal(y[T - n:], want_y) and torch.equal(nodes[T - n:], want_nodes)
+    del y, nodes
+    dy = torch.zeros_like(x)
+    dy[T - n:] = tail[1]
+    a, b = rec.gated_scan_grads(dy, None, x, r, i, decay, cu, init_states=init), rec.gated_scan_grads(tail[1], None, *tail, decay, own, init_states=init[1:])
+    for u, v in zip(a[:3], b[:3]):
+        assert float((u[T - n:].float() - v.float()).abs().max()) <= 2.0 ** -7 * float(v.float().abs().max()) and float(u[:T - n].abs().max()) == 0.0
+
+
 def test_no_tokens():
     x, decay, states = torch.zeros(0, 6, device=DEV), torch.zeros(6, device=DEV), torch.randn(2, 6, device=DEV)
     cu = _ints([0, 0, 0])
