@@ -34,41 +34,45 @@ template <typename E, int V> __global__ __launch_bounds__(kStepThreads) void rec
 // ---------------------------------------------------------------- trees
 // A wave per sequence and 64 channels, kTreeAhead tokens at a time, whose inputs are requested while those in front are worked on.  Their
 // gates, which are nearly all of the work and do not depend on states, are computed side by side; then the states, a product and
-// a sum each, those of the last kNodes tokens kept in LDS for their children (older ones are read back).  Memory latency bounds it:
-// 32 trees of 16 to 64 tokens of 4096 channels in bf16 23.5 us, of which the stores 6 and the gates 2 (two channels per thread and one
-// token at a time 26.8, four waves that share a batch's gates 34); one tree of 17 tokens 6.9 us (8.6 and 6.0).
+// a sum each, those of the last kNodes tokens kept in LDS for their children (older ones are read back).  The longest tree bounds it,
+// a batch of tokens 2 us, half of them gates on the vector units: 32 trees of 16 to 64 tokens of 4096 channels in bf16 19.8 us, 8 of
+// 256 tokens 62, one of 17 tokens 6.2 (stores and requests in branches, so that inputs are waited for together with all stores, 23.6,
+// 85 and 6.9; two channels per thread and one token at a time 26.8, 103 and 8.6; four waves that share a batch's gates 34, 78 and 6.0;
+// inputs requested two batches ahead no faster; 16 tokens at a time 20.8, 60 and 7.4).
 constexpr int kNodes = 64;
 constexpr int kTreeAhead = 8;
 template <typename E> __global__ __launch_bounds__(64) void rec_step_tree_kernel(RecIo in, const float *decay, float sharpness, int channels, const float *states, const int32_t *cu,
-                                                                                const int32_t *parents, int64_t T, void *y, int64_t y_stride, float *node_states, int nodes)
+                                                                                const int32_t *parents, int64_t T, void *y, int64_t y_stride, float *node_states)
 {
     extern __shared__ __align__(16) unsigned char lds_raw[];
-    float *const lds = reinterpret_cast<float *>(lds_raw);  // [nodes][64]
+    float *const lds = reinterpret_cast<float *>(lds_raw);  // [kNodes][64]
     const int l = threadIdx.x, b = blockIdx.y;
     const RecSeq s = rec_seq(cu, b, T);
-    const int own = blockIdx.x * 64 + l;
-    const bool c_ok = own < channels;
-    const int c = c_ok ? own : 0;
+    const int own = blockIdx.x * 64 + l, c = own < channels ? own : channels - 1;  // lanes without a channel do the last one's work once more
     if (s.n == 0)
         return;
     typedef RecRow<E, 1> Row;
     typename Row::Raw x[kTreeAhead], r[kTreeAhead], i[kTreeAhead];
-    int parent = 0;  // of token l of the present and the next ones
-    auto request = [&](int k0) __attribute__((always_inline)) {
+    int parent = 0;  // of token l of the next ones
+    auto request = [&](int from) __attribute__((always_inline)) {  // tokens behind the last one are read from that
+        const int k0 = from < s.n ? from : s.n - 1, rows = s.n - k0 < kTreeAhead ? s.n - k0 : kTreeAhead;
+        const int64_t t = s.start + (int64_t)k0;
+        const WaveRows<E> x_rows(in.x, t, in.x_stride, rows, channels), r_rows(in.r, t, in.r_stride, rows, channels), i_rows(in.i, t, in.i_stride, rows, channels);
+        const uint32_t at = x_rows.at(0, c);
 #pragma unroll
         for (int u = 0; u < kTreeAhead; ++u) {
-            const int64_t t = s.start + (int64_t)(k0 + u < s.n ? k0 + u : s.n - 1);
-            x[u] = row_load<E, 1>(in.x, t, in.x_stride, c);
-            r[u] = row_load<E, 1>(in.r, t, in.r_stride, c);
-            i[u] = row_load<E, 1>(in.i, t, in.i_stride, c);
+            const int row = u < rows ? u : rows - 1;
+            x_rows.get(at, row, x[u]);
+            r_rows.get(at, row, r[u]);
+            i_rows.get(at, row, i[u]);
         }
-        if (k0 % 64 == 0)
-            parent = parents[s.start + (int64_t)(k0 + l < s.n ? k0 + l : s.n - 1)];
+        parent = parents[t + (l < rows ? l : rows - 1)];
     };
     const float rate = decay_rate(decay[c], sharpness), root = states[(int64_t)b * channels + c];
     float h = 0.f;
     request(0);
     for (int k0 = 0; k0 < s.n; k0 += kTreeAhead) {
+        const int rows = s.n - k0 < kTreeAhead ? s.n - k0 : kTreeAhead;
         float kept[kTreeAhead], add[kTreeAhead];
         int from[kTreeAhead];
 #pragma unroll
@@ -79,32 +83,34 @@ template <typename E> __global__ __launch_bounds__(64) void rec_step_tree_kernel
             Row::unpack(i[u], &iv);
             const Gates g = gates_of(rv, iv, rate);
             kept[u] = g.a, add[u] = added(g, xv);
-            from[u] = __builtin_amdgcn_readlane(parent, (k0 + u) % 64);
+            from[u] = __builtin_amdgcn_readlane(parent, u);
         }
-        if (k0 + kTreeAhead < s.n)
-            request(k0 + kTreeAhead);
+        request(k0 + kTreeAhead);
+        const int64_t t = s.start + (int64_t)k0;
+        const WaveRows<E> y_rows(y, t, y_stride, rows, channels);
+        const WaveRows<RecF32> node_rows(node_states, t, channels, rows, channels);
+        const uint32_t y_at = y_rows.at(0, c), node_at = node_rows.at(0, c);
 #pragma unroll
         for (int u = 0; u < kTreeAhead; ++u) {
-            const int k = k0 + u, p = from[u];
-            if (k >= s.n)
-                break;
+            const int k = k0 + u, p = u < rows ? from[u] : k - 1, row = u < rows ? u : rows - 1;
             if (p != k - 1 || k == 0) {
                 h = root;
                 if (p >= 0 && p < k) {
-                    if (k - p <= nodes) {
-                        h = lds[p % nodes * 64 + l];
+                    if (k - p <= kNodes) {
+                        h = lds[(p & (kNodes - 1)) * 64 + l];
                     } else {
                         h = node_states[(s.start + (int64_t)p) * channels + c];
                         pin(h);  // waited for here: behind the branch every token would wait for all loads and stores on their way
                     }
                 }
             }
-            h = __builtin_fmaf(kept[u], h, add[u]), pin(h);
-            lds[k % nodes * 64 + l] = h;
-            if (c_ok) {
-                row_store<E, 1>(y, s.start + (int64_t)k, y_stride, own, &h);
-                node_states[(s.start + (int64_t)k) * channels + own] = h;
-            }
+            const float next = __builtin_fmaf(kept[u], h, add[u]);
+            h = u < rows ? next : h, pin(h);
+            lds[(k & (kNodes - 1)) * 64 + l] = h;
+            // No branch around the stores (behind the last token its own are repeated), nor around the requests: what waits for inputs
+            // would wait for everything behind them if their number were not known.
+            y_rows.put(y_at, row, Row::pack(&h));
+            node_rows.put(node_at, row, __float_as_uint(h));
         }
     }
 }
@@ -134,9 +140,8 @@ template <typename E, int V> hipError_t step(const rec_shape_t &s, int batch, co
 template <typename E> hipError_t step_tree(const rec_shape_t &s, int batch, int64_t T, const RecIo &in, const float *decay, const float *states, const int32_t *cu,
                                            const int32_t *parents, void *y, int64_t y_stride, float *node_states, hipStream_t stream)
 {
-    const int nodes = T < kNodes ? (int)T : kNodes;
-    hipLaunchKernelGGL((rec_step_tree_kernel<E>), dim3((unsigned)((s.channels + 63) / 64), (unsigned)batch), dim3(64), (size_t)nodes * 64 * sizeof(float), stream, in, decay,
-                       s.sharpness, s.channels, states, cu, parents, T, y, y_stride, node_states, nodes);
+    hipLaunchKernelGGL((rec_step_tree_kernel<E>), dim3((unsigned)((s.channels + 63) / 64), (unsigned)batch), dim3(64), kNodes * 64 * sizeof(float), stream, in, decay,
+                       s.sharpness, s.channels, states, cu, parents, T, y, y_stride, node_states);
     return hipGetLastError();
 }
 
