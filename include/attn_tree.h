@@ -96,7 +96,8 @@ int attn_attend_tree(const attn_shape_t *shape, int32_t batch, int64_t total_tok
  * (one value, not n_free itself) is the new length, at most free_capacity.  Only
  * rows of a sequence's own blocks may be given back (attn_assign_blocks with
  * shared_tail sees to that).  The table stays as it is; nothing reads its
- * entries behind the cached tokens before they are handed out again.
+ * entries behind the cached tokens before they are handed out again.  Without
+ * sequences nothing is written.
  */
 int attn_accept_path(int32_t batch, int32_t block_size, int32_t max_blocks, int64_t total_tokens,
                      const int32_t *tokens, const int32_t *parents, const int32_t *choices,

@@ -267,8 +267,8 @@ PyObject *accept_path(PyObject *, PyObject *const *args, Py_ssize_t n)
     const at::TensorOptions ints = tokens.options();
     const at::Tensor path = at::empty({T}, ints), counts = at::empty({batch}, ints), next_tokens = at::empty({batch}, ints), kept_lens = at::empty({batch}, ints);
     at::Tensor left;
-    if (gives_back)
-        left = at::empty({1}, ints);
+    if (gives_back)  // (nothing is enqueued for no sequences)
+        left = batch > 0 ? at::empty({1}, ints) : tensor(args[8], "n_free").clamp(0, capacity);
     check(attn_accept_path(size32(batch, "batch"), block_size, max_blocks, T, tokens_at, parents_at, choices_at, cu_at, cached_at,
                            static_cast<int32_t *>(path.data_ptr()), static_cast<int32_t *>(counts.data_ptr()), static_cast<int32_t *>(next_tokens.data_ptr()),
                            static_cast<int32_t *>(kept_lens.data_ptr()), table_at, free_at, capacity, n_free_at,

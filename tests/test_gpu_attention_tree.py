@@ -289,6 +289,18 @@ def test_no_tokens():
     attn.keep_path([], _ints([[0]]), cu, one, kept.path)
 
 
+def test_no_sequences():
+    """The free list stays as long as it is."""
+    none, cu = _ints([]), _ints([0])
+    free = _ints([5, 6, 7, -1])
+    kept = attn.accept_path(none, none, none, cu, none, block_size=16, table=torch.zeros(0, 4, dtype=torch.int32, device=DEV), free_blocks=free, n_free=_ints([3]))
+    assert [x.tolist() for x in kept] == [[], [], [], [], [3]] and free.tolist() == [5, 6, 7, -1]
+    assert attn.accept_path(none, none, none, cu, none).n_free is None
+    tree = attn.draft_tree(none, cu, none, 3)
+    assert tree.positions.shape == (0,) and tree.seen.shape == (0, 1)
+    attn.keep_path([torch.zeros(2, 2, 16, 64, device=DEV)], torch.zeros(0, 4, dtype=torch.int32, device=DEV), cu, none, none)
+
+
 def test_refusals():
     ints, cu, one = _ints([-1, 0]), _ints([0, 2]), _ints([3])
     q, cache = torch.zeros(2, 2, 64, device=DEV), torch.zeros(2, 2, 16, 64, device=DEV)
