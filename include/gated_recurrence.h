@@ -21,8 +21,8 @@
  *   rec_keep_states  the state behind the last token that was kept
  *
  * Gates, products and states are fp32; y and the gradients are rounded to the
- * type once.  A state that is not finite stays so to the end of its sequence
- * and reaches no other one.
+ * type once.  Sigmoids and 1 - a^2 below 2^-126 count as 0.  A state that is not
+ * finite stays so to the end of its sequence and reaches no other one.
  *
  * Sequence b of a packed batch is tokens cu_seqlens[b] .. cu_seqlens[b+1] - 1.
  * cu_seqlens [batch+1], int32 on the device, rises from 0 or more to at most
@@ -115,9 +115,10 @@ int rec_scan(const rec_shape_t *shape, int32_t batch, int64_t total_tokens,
  *   d_decay    [channels]  fp32 device, out
  *   d_init     [batch, channels]  fp32 device, out, or NULL
  *
- * Where a gate leaves a = 1 in fp32 (sigmoid(r) = 0), 1 - a^2 is 0 and the
- * gradients of r and decay through it are taken as 0, their limit.  Sums do not
- * depend on the timing of the GPU.
+ * Where a gate or a decay leaves 1 - a^2 below 2^-126, the smallest normal fp32
+ * value (sharpness softplus(decay) sigmoid(r) below 2^-127), it is taken as 0, and
+ * so are the gradients through it, whose limit is 0.  Sums do not depend on the
+ * timing of the GPU.
  */
 int rec_scan_grads(const rec_shape_t *shape, int32_t batch, int64_t total_tokens,
                    const void *x, int64_t x_stride, const void *r, int64_t r_stride, const void *i, int64_t i_stride,

@@ -37,6 +37,10 @@ constexpr int kGroup = 8;           // chunks of a group, and groups between pub
 constexpr uint64_t kNothing = ~0ull;
 constexpr int kMostPolls = 1 << 22; // of a wait: seconds; its result is NaN then, and the grid still drains
 constexpr float kCut = -1.f;        // A of a map that forgets what was in front: a sequence starts in it
+// Smaller 1 - a^2 are 0 to the gradients, as they are to the forward pass: the instructions for roots take denormals as 0, and the
+// reciprocal root of 0 is infinity, which times the gate's gradient, next to 0 as well, is anything.  What is dropped is at most
+// 2^-63 of what it multiplies.
+constexpr float kSmallestNormal = 0x1p-126f;
 
 // H' of a map (A, H) of `carry`, and the map of both
 __device__ __forceinline__ float apply(float2 m, float carry) { return m.x < 0.f ? m.y : __builtin_fmaf(m.x, carry, m.y); }
@@ -549,7 +553,7 @@ template <typename E, int V> __global__ __launch_bounds__(64 * kWaves, 4) void r
             for (int v = 0; v < V; ++v) {
                 const Gates &g = gates[s][v];
                 const float dh = d[v] + carry[v];
-                const float over = g.kept2 > 0.f ? __builtin_amdgcn_rsqf(g.kept2) : 0.f;
+                const float over = g.kept2 >= kSmallestNormal ? __builtin_amdgcn_rsqf(g.kept2) : 0.f;
                 const float back = g.a * dh, add = dh * (g.kept2 * over) * g.si;
                 dx[v] = add;
                 di[v] = add * xv[v] * (1.f - g.si);
