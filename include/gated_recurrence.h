@@ -30,7 +30,9 @@
  * device and nothing here allocates, copies to the host or synchronises, so
  * calls can be captured into a graph and replayed while the lengths change.  No
  * value of the device's index arrays makes a kernel access memory outside its
- * arguments.
+ * arguments.  A call takes at most 4096 sequences and 2^30 - 1 tokens, of which
+ * rec_scan and rec_scan_grads have fewer than 2^23 blocks of 64 channels by 128
+ * (rec_scan_grads: 64) tokens, of 128 channels where rows lie pair by pair.
  *
  * "device" pointers are HIP device pointers on the current device.  x, r, i, y
  * and dy are [total_tokens, channels] of io_dtype with `..._stride` elements

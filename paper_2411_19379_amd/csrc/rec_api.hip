@@ -48,12 +48,9 @@ int check_batch(int32_t batch, int64_t total_tokens)
     return REC_OK;
 }
 
-// Workgroups are numbered in 31 bits: one per 64 tokens and 64 channels.
-int check_work(const rec_shape_t &s, int64_t total_tokens)
+int check_fits(bool fits)
 {
-    if ((total_tokens / 64 + 1) * ((int64_t)s.channels / 64 + 1) > 0x7fffffff)
-        return fail(REC_ERR_UNSUPPORTED_SHAPE, "tokens times channels must be below 2^43");
-    return REC_OK;
+    return fits ? (int)REC_OK : fail(REC_ERR_UNSUPPORTED_SHAPE, "tokens and channels take more workgroups than a launch has: 2^23 - 1 of 64 channels and 128 tokens, 64 for gradients");
 }
 
 bool aligned(const void *p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -107,12 +104,13 @@ extern "C" int rec_workspace_bytes(const rec_shape_t *shape, int32_t batch, int6
     int rc = check_shape(shape);
     if (rc == REC_OK)
         rc = check_batch(batch, total_tokens);
-    if (rc == REC_OK)
-        rc = check_work(*shape, total_tokens);
     if (rc != REC_OK)
         return rc;
     if (!bytes || grads < 0 || grads > 2)
         return fail(REC_ERR_INVALID_ARG, "bytes is NULL or grads not one of 0, 1, 2");
+    rc = check_fits(rec_fits(*shape, total_tokens, grads));
+    if (rc != REC_OK)
+        return rc;
     *bytes = rec_scan_workspace(*shape, batch, total_tokens, grads);
     return REC_OK;
 }
@@ -125,8 +123,6 @@ extern "C" int rec_scan(const rec_shape_t *shape, int32_t batch, int64_t total_t
     int rc = check_shape(shape);
     if (rc == REC_OK)
         rc = check_batch(batch, total_tokens);
-    if (rc == REC_OK)
-        rc = check_work(*shape, total_tokens);
     if (rc != REC_OK)
         return rc;
     if (n_ckpt < 0 || (n_ckpt > 0 && (!ckpt || !ckpt_states)))
@@ -135,6 +131,11 @@ extern "C" int rec_scan(const rec_shape_t *shape, int32_t batch, int64_t total_t
         return fail(REC_ERR_MISALIGNED, "a device pointer is not aligned to its type");
     if (batch == 0)
         return n_ckpt == 0 ? (int)REC_OK : fail(REC_ERR_INVALID_ARG, "checkpoints without sequences");
+    RecScan a;
+    a.in = RecIo{x, r, i, x_stride, r_stride, i_stride};
+    a.decay = decay, a.init = init_states, a.cu = cu_seqlens, a.ckpt = ckpt;
+    a.y = y, a.y_stride = y_stride, a.final_states = final_states, a.ckpt_states = ckpt_states, a.saved = saved;
+    a.T = total_tokens, a.batch = batch, a.n_ckpt = n_ckpt;
     if (total_tokens > 0) {
         rc = check_inputs(*shape, x, x_stride, r, r_stride, i, i_stride);
         if (rc == REC_OK && y)
@@ -142,15 +143,12 @@ extern "C" int rec_scan(const rec_shape_t *shape, int32_t batch, int64_t total_t
         if (rc == REC_OK && (!decay || !cu_seqlens))
             rc = fail(REC_ERR_INVALID_ARG, "decay or cu_seqlens is NULL");
         if (rc == REC_OK)
+            rc = check_fits(rec_fits(*shape, a));
+        if (rc == REC_OK)
             rc = check_workspace(*shape, batch, total_tokens, 0, workspace, workspace_bytes);
         if (rc != REC_OK)
             return rc;
     }
-    RecScan a;
-    a.in = RecIo{x, r, i, x_stride, r_stride, i_stride};
-    a.decay = decay, a.init = init_states, a.cu = cu_seqlens, a.ckpt = ckpt;
-    a.y = y, a.y_stride = y_stride, a.final_states = final_states, a.ckpt_states = ckpt_states, a.saved = saved;
-    a.T = total_tokens, a.batch = batch, a.n_ckpt = n_ckpt;
     return hip_status(launch_rec_scan(*shape, a, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -163,14 +161,17 @@ extern "C" int rec_scan_grads(const rec_shape_t *shape, int32_t batch, int64_t t
     int rc = check_shape(shape);
     if (rc == REC_OK)
         rc = check_batch(batch, total_tokens);
-    if (rc == REC_OK)
-        rc = check_work(*shape, total_tokens);
     if (rc != REC_OK)
         return rc;
     if (!decay || !d_decay)
         return fail(REC_ERR_INVALID_ARG, "decay or d_decay is NULL");
     if (!floats({decay, init_states, saved, d_final, d_decay, d_init}))
         return fail(REC_ERR_MISALIGNED, "a device pointer is not aligned to its type");
+    RecGrads a;
+    a.in = RecIo{x, r, i, x_stride, r_stride, i_stride};
+    a.decay = decay, a.init = init_states, a.saved = saved, a.d_final = d_final, a.cu = cu_seqlens;
+    a.dy = dy, a.dy_stride = dy_stride, a.dx = dx, a.dr = dr, a.di = di, a.d_decay = d_decay, a.d_init = d_init;
+    a.T = total_tokens, a.batch = batch;
     if (total_tokens > 0) {
         rc = check_inputs(*shape, x, x_stride, r, r_stride, i, i_stride);
         if (rc == REC_OK && dy)
@@ -181,15 +182,12 @@ extern "C" int rec_scan_grads(const rec_shape_t *shape, int32_t batch, int64_t t
         if (rc == REC_OK && !cu_seqlens)
             rc = fail(REC_ERR_INVALID_ARG, "cu_seqlens is NULL");
         if (rc == REC_OK)
+            rc = check_fits(rec_fits(*shape, a));
+        if (rc == REC_OK)
             rc = check_workspace(*shape, batch, total_tokens, saved ? 1 : 2, workspace, workspace_bytes);
         if (rc != REC_OK)
             return rc;
     }
-    RecGrads a;
-    a.in = RecIo{x, r, i, x_stride, r_stride, i_stride};
-    a.decay = decay, a.init = init_states, a.saved = saved, a.d_final = d_final, a.cu = cu_seqlens;
-    a.dy = dy, a.dy_stride = dy_stride, a.dx = dx, a.dr = dr, a.di = di, a.d_decay = d_decay, a.d_init = d_init;
-    a.T = total_tokens, a.batch = batch;
     return hip_status(launch_rec_grads(*shape, a, workspace, static_cast<hipStream_t>(hip_stream)));
 }
 

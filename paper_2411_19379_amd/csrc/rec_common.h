@@ -186,6 +186,10 @@ struct RecGrads {
 };
 // Launchers implemented next to their kernels.
 size_t rec_scan_workspace(const rec_shape_t &s, int batch, int64_t T, int grads);
+// Whether a launch can number the workgroups of T tokens, where rows allow the most channels in each, and of these rows.
+bool rec_fits(const rec_shape_t &s, int64_t T, int grads);
+bool rec_fits(const rec_shape_t &s, const RecScan &a);
+bool rec_fits(const rec_shape_t &s, const RecGrads &a);
 hipError_t launch_rec_scan(const rec_shape_t &s, const RecScan &a, void *workspace, hipStream_t stream);
 hipError_t launch_rec_grads(const rec_shape_t &s, const RecGrads &a, void *workspace, hipStream_t stream);
 hipError_t launch_rec_step(const rec_shape_t &s, int batch, const RecIo &in, const float *decay, float *states, void *y, int64_t y_stride,

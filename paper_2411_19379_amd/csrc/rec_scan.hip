@@ -694,6 +694,7 @@ hipError_t prepare(const rec_shape_t &s, const Workspace &w, const Look &look, c
 }
 
 bool pairs(const void *p, int64_t stride, int bytes) { return reinterpret_cast<uintptr_t>(p) % (2 * bytes) == 0 && stride % 2 == 0; }
+int64_t workgroups(const rec_shape_t &s, int64_t T, bool two, int chunk) { return (s.channels + (two ? 127 : 63)) / (two ? 128 : 64) * ((T + chunk - 1) / chunk); }
 // Two channels per lane, half of the loads, where rows allow it and more than REC_FEW_WORKGROUPS are left: with one there are twice as
 // many, which 256 compute units can all run at once (us, one channel and two; bf16, 1000 channels, scan of 1600 tokens, 104 workgroups,
 // 14.0 and 15.8, of 3200, 200, 19.6 and 17.8, of 32768 tokens of 4096 channels 293 and 264; gradients of 800 tokens, 104, 16.7 and
@@ -701,9 +702,29 @@ bool pairs(const void *p, int64_t stride, int bytes) { return reinterpret_cast<u
 bool two_channels(const rec_shape_t &s, const RecIo &in, int64_t T, int chunk)
 {
     const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
-    return s.channels % 2 == 0 && (s.channels + 127) / 128 * ((T + chunk - 1) / chunk) > REC_FEW_WORKGROUPS && pairs(in.x, in.x_stride, e) && pairs(in.r, in.r_stride, e) &&
-           pairs(in.i, in.i_stride, e);
+    return s.channels % 2 == 0 && workgroups(s, T, true, chunk) > REC_FEW_WORKGROUPS && pairs(in.x, in.x_stride, e) && pairs(in.r, in.r_stride, e) && pairs(in.i, in.i_stride, e);
 }
+constexpr int kScanChunk = Place<1, kScanTokens>::kChunk, kGradsChunk = Place<1, kGradsTokens>::kChunk;
+bool scan_two(const rec_shape_t &s, const RecScan &a)
+{
+    const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
+    return two_channels(s, a.in, a.T, kScanChunk) && pairs(a.init, 0, 4) && (!a.y || pairs(a.y, a.y_stride, e)) && pairs(a.final_states, 0, 4) && pairs(a.ckpt_states, 0, 4) &&
+           pairs(a.saved, 0, 4);
+}
+// fp32: rows of one channel per lane are 256 bytes already (12800 tokens of 2560 channels 209 us, two channels 232)
+bool grads_two(const rec_shape_t &s, const RecGrads &a)
+{
+    return s.io_dtype != REC_DT_F32 && two_channels(s, a.in, a.T, kGradsChunk) && pairs(a.init, 0, 4) && (!a.dy || pairs(a.dy, a.dy_stride, 2)) && pairs(a.saved, 0, 4) &&
+           pairs(a.d_final, 0, 4) && pairs(a.dx, 0, 2) && pairs(a.dr, 0, 2) && pairs(a.di, 0, 2) && pairs(a.d_init, 0, 4);
+}
+// The forward pass that computes again what the backward pass is not given.
+RecScan again_of(const RecGrads &a)
+{
+    RecScan f = {};
+    f.in = a.in, f.decay = a.decay, f.init = a.init, f.cu = a.cu, f.T = a.T, f.batch = a.batch;
+    return f;
+}
+constexpr int64_t kMostWorkgroups = 0xffffffffll / (64 * kWaves);  // a launch numbers its threads in 32 bits
 
 template <typename K> hipError_t lds_limit(K kernel, size_t lds)
 {
@@ -755,9 +776,19 @@ size_t rec_scan_workspace(const rec_shape_t &s, int batch, int64_t T, int grads)
 {
     if (T == 0 || batch == 0)
         return 0;
-    const size_t scan = Workspace(s.channels, T, Place<1, kScanTokens>::kChunk, 0).bytes;
-    const size_t all = grads ? Workspace(s.channels, T, Place<1, kGradsTokens>::kChunk, grads).bytes : 0;
+    const size_t scan = Workspace(s.channels, T, kScanChunk, 0).bytes;
+    const size_t all = grads ? Workspace(s.channels, T, kGradsChunk, grads).bytes : 0;
     return scan > all ? scan : all;
+}
+
+bool rec_fits(const rec_shape_t &s, int64_t T, int grads)
+{
+    return workgroups(s, T, s.channels % 2 == 0 && !(grads && s.io_dtype == REC_DT_F32), grads ? kGradsChunk : kScanChunk) <= kMostWorkgroups;
+}
+bool rec_fits(const rec_shape_t &s, const RecScan &a) { return workgroups(s, a.T, scan_two(s, a), kScanChunk) <= kMostWorkgroups; }
+bool rec_fits(const rec_shape_t &s, const RecGrads &a)
+{
+    return workgroups(s, a.T, grads_two(s, a), kGradsChunk) <= kMostWorkgroups && (a.saved || rec_fits(s, again_of(a)));
 }
 
 hipError_t launch_rec_scan(const rec_shape_t &s, const RecScan &a, void *workspace, hipStream_t stream)
@@ -767,9 +798,7 @@ hipError_t launch_rec_scan(const rec_shape_t &s, const RecScan &a, void *workspa
         return e != hipSuccess ? e : copy_states(a.ckpt_states, nullptr, (int64_t)a.n_ckpt * s.channels, stream);
     }
     unsigned char *const at = static_cast<unsigned char *>(workspace);
-    const int e = s.io_dtype == REC_DT_F32 ? 4 : 2;
-    const bool two = two_channels(s, a.in, a.T, Place<2, kScanTokens>::kChunk) && pairs(a.init, 0, 4) && (!a.y || pairs(a.y, a.y_stride, e)) && pairs(a.final_states, 0, 4) && pairs(a.ckpt_states, 0, 4) &&
-                     pairs(a.saved, 0, 4);
+    const bool two = scan_two(s, a);
     if (s.io_dtype == REC_DT_F32)
         return two ? scan<RecF32, 2>(s, a, at, stream) : scan<RecF32, 1>(s, a, at, stream);
     if (s.io_dtype == REC_DT_BF16)
@@ -786,16 +815,12 @@ hipError_t launch_rec_grads(const rec_shape_t &s, const RecGrads &given, void *w
     }
     unsigned char *const at = static_cast<unsigned char *>(workspace);
     const bool again = !a.saved;
-    // fp32: rows of one channel per lane are 256 bytes already (12800 tokens of 2560 channels 209 us, two channels 232)
-    const bool two = s.io_dtype != REC_DT_F32 && two_channels(s, a.in, a.T, Place<2, kGradsTokens>::kChunk) && pairs(a.init, 0, 4) &&
-                     (!a.dy || pairs(a.dy, a.dy_stride, 2)) && pairs(a.saved, 0, 4) && pairs(a.d_final, 0, 4) && pairs(a.dx, 0, 2) && pairs(a.dr, 0, 2) &&
-                     pairs(a.di, 0, 2) && pairs(a.d_init, 0, 4);
-    const Workspace w(s.channels, a.T, Place<1, kGradsTokens>::kChunk, again ? 2 : 1);
+    const bool two = grads_two(s, a);
+    const Workspace w(s.channels, a.T, kGradsChunk, again ? 2 : 1);
     if (again) {
         // its maps lie in front of what it saves
-        const size_t maps = Workspace(s.channels, a.T, Place<1, kScanTokens>::kChunk, 0).bytes;
-        RecScan f = {};
-        f.in = a.in, f.decay = a.decay, f.init = a.init, f.cu = a.cu, f.T = a.T, f.batch = a.batch;
+        const size_t maps = Workspace(s.channels, a.T, kScanChunk, 0).bytes;
+        RecScan f = again_of(a);
         f.saved = reinterpret_cast<float *>(at + (w.saved > maps ? w.saved : maps));
         a.saved = f.saved;
         const hipError_t e = launch_rec_scan(s, f, workspace, stream);
