@@ -14,7 +14,8 @@ A step that checks trees of drafted tokens has, with `step` as above,
 
 All of it is enqueued on the current torch stream, nothing waits for the GPU, and lengths are read there; outputs and the
 workspace are torch tensors.  There is no CPU fallback: loading raises if the library has not been built.  There is no backward
-pass either: where a graph is recorded, tensors that require grad are refused (serve under `torch.no_grad()`).
+pass either: where a graph is recorded, tensors that require grad are refused (serve under `torch.no_grad()`), and tensors with a
+tangent of forward-mode differentiation always.
 """
 from __future__ import annotations
 

@@ -288,19 +288,21 @@ PyObject *keep_path(PyObject *, PyObject *const *args, Py_ssize_t n)
     const bool list = PyList_Check(args[0]);
     const Py_ssize_t n_caches = list ? PyList_GET_SIZE(args[0]) : PyTuple_GET_SIZE(args[0]);
     TORCH_CHECK_VALUE(n_caches <= 256, "caches: at most 256 per call, got ", n_caches);
+    const at::Tensor *caches[256];
+    for (Py_ssize_t c = 0; c < n_caches; ++c) {
+        caches[c] = &tensor(list ? PyList_GET_ITEM(args[0], c) : PyTuple_GET_ITEM(args[0], c), "caches");
+        no_gradients({{"a cache", caches[c]}});
+    }
     const at::Tensor &table = tensor(args[1], "table"), &cu = tensor(args[2], "cu_seqlens"), &cached = tensor(args[3], "cached_lens"), &path = tensor(args[4], "path");
     const int device = on_current_device(path);
     const int64_t T = path.numel(), batch = cu.numel() - 1;
     const int32_t *table_at = address<int32_t>("table", table, {batch, -1}, at::kInt, device), *cu_at = address<int32_t>("cu_seqlens", cu, {-1}, at::kInt, device);
     const int32_t *cached_at = address<int32_t>("cached_lens", cached, {batch}, at::kInt, device), *path_at = address<int32_t>("path", path, {-1}, at::kInt, device);
-    const at::Tensor *caches[256];
     void *at_[256];
     attn_shape_t s = {};
     int32_t n_blocks = 0;
     for (Py_ssize_t c = 0; c < n_caches; ++c) {
-        caches[c] = &tensor(list ? PyList_GET_ITEM(args[0], c) : PyTuple_GET_ITEM(args[0], c), "caches");
         const at::Tensor &x = *caches[c], &first = *caches[0];
-        no_gradients({{"a cache", &x}});
         TORCH_CHECK_VALUE(x.dim() == 4, "caches: expected [n_blocks, n_kv_heads, block_size, head_dim], got ", x.sizes());
         at_[c] = address("caches", x, {first.size(0), first.size(1), first.size(2), first.size(3)}, first.scalar_type(), device);
     }

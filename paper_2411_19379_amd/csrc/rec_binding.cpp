@@ -67,12 +67,13 @@ at::Tensor workspace_of(const Inputs &in, int64_t batch, int grads)
     check(rec_workspace_bytes(&in.shape, size32(batch, "batch"), in.T, grads, &need));
     return at::empty({(int64_t)need}, in.options.dtype(at::kByte));
 }
-void no_graph(PyObject *const *args, std::initializer_list<const char *> names)
+typedef void Refusal(std::initializer_list<Named>);
+void none_of(Refusal *refusal, PyObject *const *args, std::initializer_list<const char *> names)
 {
     int k = 0;
     for (const char *name : names) {
         if (args[k] != Py_None)
-            no_gradients({{name, &tensor(args[k], name)}});
+            refusal({{name, &tensor(args[k], name)}});
         ++k;
     }
 }
@@ -82,6 +83,9 @@ PyObject *scan(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     arguments(n, 10);
+    none_of(no_tangents, args, {"x", "r", "i", "decay"});
+    none_of(no_tangents, args + 6, {"init_states"});
+    none_of(no_tangents, args + 8, {"out"});
     const Inputs in = inputs(args, args[5]);
     const at::Tensor &cu = tensor(args[4], "cu_seqlens");
     const int32_t *cu_at = address<int32_t>("cu_seqlens", cu, {-1}, at::kInt, in.device);
@@ -122,6 +126,8 @@ PyObject *scan_grads(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     arguments(n, 11);
+    none_of(no_tangents, args, {"x", "r", "i", "decay"});
+    none_of(no_tangents, args + 6, {"init_states", "saved", "dy", "d_final"});
     const Inputs in = inputs(args, args[5]);
     const at::Tensor &cu = tensor(args[4], "cu_seqlens");
     const int32_t *cu_at = address<int32_t>("cu_seqlens", cu, {-1}, at::kInt, in.device);
@@ -153,8 +159,8 @@ PyObject *step(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     arguments(n, 7);
-    no_graph(args, {"x", "r", "i", "decay", "states"});
-    no_graph(args + 6, {"out"});
+    none_of(no_gradients, args, {"x", "r", "i", "decay", "states"});
+    none_of(no_gradients, args + 6, {"out"});
     const Inputs in = inputs(args, args[5]);
     const at::Tensor &states = tensor(args[4], "states");
     float *states_at = address<float>("states", states, {in.T, in.shape.channels}, at::kFloat, in.device);
@@ -174,8 +180,8 @@ PyObject *step_tree(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     arguments(n, 9);
-    no_graph(args, {"x", "r", "i", "decay", "states"});
-    no_graph(args + 8, {"out"});
+    none_of(no_gradients, args, {"x", "r", "i", "decay", "states"});
+    none_of(no_gradients, args + 8, {"out"});
     const Inputs in = inputs(args, args[7]);
     const at::Tensor &cu = tensor(args[5], "cu_seqlens");
     const int32_t *cu_at = address<int32_t>("cu_seqlens", cu, {-1}, at::kInt, in.device);
@@ -199,7 +205,7 @@ PyObject *keep_states(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
     arguments(n, 5);
-    no_graph(args, {"states", "node_states"});
+    none_of(no_gradients, args, {"states", "node_states"});
     const at::Tensor &states = tensor(args[0], "states"), &nodes = tensor(args[1], "node_states"), &cu = tensor(args[2], "cu_seqlens"), &path = tensor(args[3], "path");
     const int device = on_current_device(states);
     TORCH_CHECK_VALUE(states.dim() == 2, "states: expected [batch, channels], got ", states.sizes());

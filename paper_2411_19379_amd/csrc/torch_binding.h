@@ -4,6 +4,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -71,13 +72,23 @@ template <typename T = void> T *address(const char *name, const at::Tensor &t, s
     return static_cast<T *>(t.data_ptr());
 }
 
-// There is no backward pass: where a graph is recorded, a result outside it would drop gradients in silence.
 struct Named {
     const char *name;
     const at::Tensor *t;
 };
+// Nothing hands on the tangents of forward-mode differentiation, which torch.no_grad() does not stop: a result without one would drop
+// it in silence.
+void no_tangents(std::initializer_list<Named> all)
+{
+    if (!c10::AutogradState::get_tls_state().get_fw_grad_mode())
+        return;
+    for (const Named &n : all)
+        TORCH_CHECK_VALUE(!n.t->_fw_grad(0).defined(), n.name, " has a tangent, and this operator has no forward-mode derivative: detach it");
+}
+// There is no backward pass: where a graph is recorded, a result outside it would drop gradients in silence.
 void no_gradients(std::initializer_list<Named> all)
 {
+    no_tangents(all);
     if (!c10::GradMode::is_enabled())
         return;
     for (const Named &n : all)

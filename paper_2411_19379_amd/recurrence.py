@@ -9,7 +9,8 @@
 
 x, r, i and y are [tokens, channels] in float32, bfloat16 or float16; decay [channels] and all states are float32.  All of it is
 enqueued on the current torch stream and nothing waits for the GPU.  There is no CPU fallback: loading raises if the library
-has not been built.  `gated_scan` records a graph where an input requires grad; the others refuse such tensors.
+has not been built.  `gated_scan` records a graph where an input requires grad; the others refuse such tensors, and all refuse those
+with a tangent of forward-mode differentiation.
 """
 from __future__ import annotations
 
