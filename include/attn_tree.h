@@ -64,7 +64,9 @@ int attn_tree_workspace_bytes(const attn_shape_t *shape, int32_t batch, int64_t 
  *       not only those of attn_draft_tree
  *
  * Positions are cut to cached_lens[b] .. cached_lens[b] + i.  positions may not
- * be NULL; seen is [total_tokens, words], words 1 to 32.
+ * be NULL; seen is [total_tokens, words], words 1 to 32.  max_new decides more
+ * here: 33 to 256 rows of heads per key head have a kernel of their own, and
+ * 0 counts all tokens as one sequence's.
  */
 int attn_attend_tree(const attn_shape_t *shape, int32_t batch, int64_t total_tokens, int32_t n_blocks, int32_t max_blocks,
                      const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,

@@ -84,7 +84,9 @@ int rec_workspace_bytes(const rec_shape_t *shape, int32_t batch, int64_t total_t
  *   decay         [channels]  fp32 device
  *   init_states   [batch, channels]  fp32 device, or NULL: zeros
  *   ckpt          [n_ckpt]  int32 device: packed tokens whose states are wanted,
- *                 in any order, more than once if need be; NULL if n_ckpt is 0
+ *                 in any order, more than once if need be; NULL if n_ckpt is 0.
+ *                 Each is looked for among all: some hundreds per call cost
+ *                 little, thousands many times the scan
  *   y             io_dtype, or NULL: not wanted.  Rows of tokens of no sequence
  *                 are not written.
  *   final_states  [batch, channels]  fp32 device, out, or NULL: behind a

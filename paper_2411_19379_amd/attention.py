@@ -8,7 +8,7 @@ A step that checks trees of drafted tokens has, with `step` as above,
 
     tree = draft_tree(parents, cu_seqlens, cached_lens, max_new)                                          # once per step
     q = rope_append(q, k, v, tree.positions, step.slots, rotary, k_cache, v_cache, copies=step.copies)    # once per layer
-    out = attend_tree(q, k_cache, v_cache, step.table, cu_seqlens, cached_lens, tree.positions, tree.seen)
+    out = attend_tree(q, k_cache, v_cache, step.table, cu_seqlens, cached_lens, tree.positions, tree.seen, max_new=max_new)
     kept = accept_path(tokens, parents, choices, cu_seqlens, cached_lens, ...)                            # behind the model
     keep_path(caches, step.table, cu_seqlens, cached_lens, kept.path)                                     # all layers
 
@@ -191,7 +191,9 @@ def draft_tree(parents, cu_seqlens, cached_lens, max_new: int, *, window: int = 
 def attend_tree(q, k_cache, v_cache, table, cu_seqlens, cached_lens, positions, seen, *, scale: Optional[float] = None,
                 window: int = 0, sinks: int = 0, max_new: int = 0, out=None, return_lse: bool = False):
     """`attend` where the new tokens are trees: cached keys are seen by `positions`, a sequence's new tokens by the bits of
-    `seen`, which need not come from `draft_tree`: a row may have any bits up to its own token's, or none."""
+    `seen`, which need not come from `draft_tree`: a row may have any bits up to its own token's, or none.  Without `max_new` all
+    tokens are taken to be one sequence's, as a rule for a kernel that is made for more rows (32 trees of 16 to 64 tokens over
+    114453 cached keys 229 us, with it 162)."""
     return (_binding or _native()).attend_tree(q, k_cache, v_cache, table, cu_seqlens, cached_lens, positions, seen, scale, window,
                                                sinks, max_new, out, return_lse)
 

@@ -21,7 +21,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const int32_t *cu, const int32_t *ca
 // depth(i) = depth(p(i)) + 1, position = cached + depth;  seen(i) = {i} u seen(p(i)), of which a window leaves the near ones and the
 // sinks.  A workgroup per sequence, its parents in LDS, a thread per token that walks up to the root: ancestors come in falling
 // order, so a thread has one word of its bits in hand at a time.  All latency: the lengths, the parents, a walk of some 100 cycles
-// per ancestor.
+// per ancestor, with a window a second one in front that counts them.
 constexpr int kDraftThreads = 256;
 
 __global__ __launch_bounds__(kDraftThreads) void attn_draft_tree_kernel(int batch, int64_t T, int words, const int32_t *parents, const int32_t *cu,
@@ -81,9 +81,10 @@ __global__ __launch_bounds__(kDraftThreads) void attn_draft_tree_kernel(int batc
 // ---------------------------------------------------------------- the branch that is kept
 // v_0 is the sequence's first token, v_(k+1) the first child of v_k that is the token chosen behind v_k.  A wave per sequence, a token
 // per lane and 64 at a time: children come behind their parents, so one walk over the tokens finds the branch.  One workgroup for the
-// batch, since the blocks that are given back go to the free list in the order of the sequences; a wave has the tokens of up
-// to kAcceptAtOnce sequences on their way at once.  Latency bounds it: a launch, four trips to memory and two barriers; one tree 4.5 us,
-// 64 trees of 16 to 64 tokens 12 us (walking four sequences side by side, with the blocks kept in registers, 11.7).
+// batch, since the blocks that are given back go to the free list in the order of the sequences and their places are a sum over those
+// in front (the walks would not need it: every further 64 trees are one more pass); a wave has the tokens of up to kAcceptAtOnce
+// sequences on their way at once.  Latency bounds it: a launch, four trips to memory and two barriers; one tree 4.5 us, 64 trees of 16
+// to 64 tokens 12 us (walking four sequences side by side, with the blocks kept in registers, 11.7).
 constexpr int kAcceptThreads = 1024;
 constexpr int kAcceptWaves = kAcceptThreads / 64;
 constexpr int kAcceptAtOnce = 4;
@@ -225,9 +226,10 @@ __global__ __launch_bounds__(kAcceptThreads) void attn_accept_kernel(AcceptArgs 
 
 // ---------------------------------------------------------------- keys and values of the branch
 // Row cached + path[k] of every cache goes to row cached + k.  path[k] >= k and rises, so in rising order no row is overwritten
-// before it has been read; a thread has the same 16 bytes of all rows and keeps that order, kKeepAtOnce rows at a time.  Where the
-// rows lie is looked up by a lane per kept token, 64 at once: lengths, path, table and rows are four trips to memory (with every
-// thread looking up its rows, eight at a time, 64 trees and 16 caches took 8.9 us, so 5.7).
+// before it has been read; a thread has the same 16 bytes of all rows and keeps that order.  Where the rows lie is looked up by a lane
+// per kept token, 64 at once: lengths, path and table are three trips to memory (with every thread looking up its rows, eight at a
+// time, 64 trees and 16 caches took 8.9 us, so 5.7).  Rows are written as kKeepAtOnce at a time, but the compiler keeps them in
+// scratch memory, 144 bytes per lane, as their loads are in branches: each is waited for, written there and read back.
 constexpr int kKeepThreads = 256;
 constexpr int kKeepAtOnce = 8;
 

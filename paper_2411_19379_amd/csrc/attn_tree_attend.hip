@@ -335,11 +335,12 @@ struct TreeChoice {
     Launch launch;
     int waves;  // 0: a kernel of attn_attend.hip
 };
-// By the most rows that a sequence may have (us, times against those of the kernels of attn_attend.hip):  up to 32 the kernel for few
-// rows is faster anyway;  up to 64 two waves (32 trees of 8 to 16 tokens and groups of 4 heads over 512 to 8192 keys 117, 146);  up to
-// 128 four (64 trees of 32 tokens 171, 215; one of 17 over 4011 keys 20.5, 22.1);  up to 256 two tiles of four waves, whose keys come
-// from memory once and from the L2 again, where there are sequences and key heads for every compute unit (32 trees of 16 to 64 tokens
-// 162, 229), else the kernel for chunks (8 trees of 64 tokens 66, 57; one 37, 32), as for more rows.
+// By the most rows that a sequence may have (us, times against those of the kernels of attn_attend.hip; 32 heads and 8 key heads of 128
+// values in bf16, 32 trees over 114453 cached keys in all, 64 over 136644, 8 over 27462):  up to 32 the kernel for few rows is faster
+// anyway;  up to 64 two waves (32 trees of 8 to 16 tokens 117, 146);  up to 128 four (64 trees of 32 tokens 171, 215; one of 17 over
+// 4011 keys 20.5, 22.1);  up to 256 two tiles of four waves, whose keys come from memory once and from the L2 again, where there are
+// sequences and key heads for every compute unit (32 trees of 16 to 64 tokens 162, 229; others over 86418 keys 119), else the kernel
+// for chunks (8 trees of 64 tokens 66, 57; one 37, 32), as for more rows.
 //
 // A partial result of 64 rows costs as much memory time as 4 tiles: where sequences and key heads alone are work enough, pieces get at
 // least 24 tiles (32 trees of 16 to 64 tokens 162, with 8 and shared by 768 workgroups 188), else 6.  Four waves are shared by 400

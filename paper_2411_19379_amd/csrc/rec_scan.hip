@@ -16,7 +16,8 @@
 //
 // Memory bounds long batches, and beside it the wait for the state in front, 30 to 50 us of the first: a prompt of 32768 tokens of 4096
 // channels in bf16 265 us, 1.09 GB at 4.1 TB/s where copies reach 4.9, vector units busy 53 % of the time;  13877 tokens of 2560
-// channels forwards 73 us, 3.8 TB/s, backwards 139 us, 0.55 GB at 3.9 TB/s, vector units 40 %.  (One level of published maps and chunks
+// channels forwards 73 us, 3.8 TB/s, backwards 139 us, 0.55 GB at 3.9 TB/s, vector units 40 %; with two channels per lane the backward
+// pass has more than its 128 registers hold, and 50 MB of what it writes, and as much of what it reads, is scratch memory.  (One level of published maps and chunks
 // of 64 tokens: 293, 85 and 219 us.)  Short ones are latency: a launch that empties the words, a ticket, lengths, inputs, two
 // or three waits for words, 11 us for 800 tokens of 256 channels.
 #include <cmath>
